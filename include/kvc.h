@@ -289,6 +289,110 @@ long long kvc_launch_count(const kvc_ctx* ctx);
 /* Text of the most recent error of this context (never NULL; valid until the next call). */
 const char* kvc_last_error(const kvc_ctx* ctx);
 
+/* ====================================================================================================================
+ * A pool of pages: answering from retained caches.  (No counterpart in the paper, whose method ends with the compressed
+ * caches: what a program does with them next.)
+ *
+ * The caches of many requests live in pages of `page_size` tokens.  A pool describes the shape; the caller owns one blob of
+ * device memory per layer, the page tables and the lengths.  Notation: P = page_size, N = n_pages, G = Hq / Hkv.
+ *
+ *   slot       page * P + row: the place of one token (all its kv-heads) in a blob
+ *   blob       K [N][Hkv][P][d], V [N][Hkv][P][d] in dtype (KVC_PAGES_PLAIN), or 8-bit codes followed by their scales
+ *              K, V [N][Hkv][P][d] int8, K, V scales [N][Hkv][P] fp32, each part at a multiple of 256 bytes (KVC_PAGES_INT8)
+ *   8 bits     a row x[0..d) of one token and kv-head is held as codes c = rint(x / s) in [-127, 127], s = max|x| / 127, and
+ *              stands for s * c.  A row whose s is below the smallest normal fp32 number is held as zeros; one with an infinity
+ *              or a NaN in it has s = NaN, so it reads back as NaN and does not pass for a number.
+ *   table      DEVICE int32 [n_seqs][table_stride]: the pages of sequence i, in order.  Entries behind the last page that its
+ *              length reaches are not read.
+ *
+ * A sequence's rows need not be all tokens of it: a compressed cache holds the retained ones (keys carry their positions, so
+ * attention does not ask for their order).  Lengths are read on the device: a captured graph may be replayed as they grow.
+ * What a call cannot check on the host it checks on the device: a slot or page outside the pool, or a length beyond the table, is
+ * left out and leaves KVC_EINVAL in the workspace's status word (kvc_pool_status).  Calls that share a workspace must be ordered
+ * on one stream.
+ * Calls only enqueue work on `stream`; pointers to rows are 16-byte aligned, row strides are multiples of 16 bytes and at least the
+ * row itself, and every tensor's innermost dimension is contiguous. */
+typedef struct kvc_pool kvc_pool; /* opaque, host memory */
+
+typedef enum { KVC_PAGES_PLAIN = 0, KVC_PAGES_INT8 = 1 } kvc_page_format;
+
+typedef struct {
+  int n_q_heads;       /* Hq, multiple of n_kv_heads, at most 128 times as many              */
+  int n_kv_heads;      /* Hkv                                                                */
+  int head_dim;        /* d in {64, 128}                                                     */
+  int dtype;           /* kvc_dtype of q/k/v/out, and of plain pages                         */
+  int page_format;     /* kvc_page_format                                                    */
+  int page_size;       /* P: 16, 32, 64, 128 or 256 tokens                                   */
+  int n_pages;         /* N >= 1                                                             */
+  int max_seqs;        /* most sequences of one kvc_pool_decode call                         */
+  float softmax_scale; /* 0 -> 1/sqrt(head_dim)                                              */
+  int device;          /* CUDA device ordinal                                                */
+  unsigned flags;      /* 0                                                                  */
+} kvc_pool_config;
+
+/* Validates the configuration and creates the host object.  *out is set to NULL on failure.  Allocates no device memory. */
+int kvc_pool_create(const kvc_pool_config* cfg, kvc_pool** out);
+int kvc_pool_destroy(kvc_pool* pool);
+
+/* Bytes of device memory the caller provides: per_layer = one layer's blob, workspace = scratch shared by all layers (both
+ * 256-byte aligned).  Either pointer may be NULL. */
+int kvc_pool_nbytes(const kvc_pool* pool, size_t* per_layer, size_t* workspace);
+
+/* Clears the status word and the scratch counters.  Call once after allocating a workspace.  Asynchronous on `stream`. */
+int kvc_pool_workspace_init(kvc_pool* pool, void* workspace, void* stream);
+
+/* Writes n tokens' rows into slots, quantised if the pages are in 8 bits.
+ *   k, v   DEVICE, row (token t, kv-head h) at t * token_stride + h * head_stride ELEMENTS: rows as a projection leaves them
+ *          ([n][Hkv][d], also inside a wider row) or as a retained cache holds them ([Hkv][cap][d], kvc_view)
+ *   slots  DEVICE int64 [n]; a negative slot skips its token; which of two tokens with one slot stays is unspecified */
+int kvc_pool_write(kvc_pool* pool, const void* k, const void* v, long long token_stride, long long head_stride,
+                   const long long* slots, long long n, void* blob, void* workspace, void* stream);
+
+/* Reads slots back as rows of dtype (strides as in kvc_pool_write; rows must not overlap).  A negative slot, or one outside the
+ * pool, gives zeros. */
+int kvc_pool_read(kvc_pool* pool, const void* blob, const long long* slots, long long n, void* k, void* v,
+                  long long token_stride, long long head_stride, void* workspace, void* stream);
+
+/* Attention of one new token per sequence over the rows its pages hold:
+ *   out[i][h] = softmax_j(scale q[i][h] . k_j) v_j over rows j < lens[i], and over the token itself if k_new is given.
+ *   q            DEVICE, row i (Hq heads of d, contiguous) at i * q_stride ELEMENTS
+ *   k_new, v_new DEVICE, row i (Hkv heads of d, contiguous) at i * kv_stride; both NULL or both given.  Then the token's row is
+ *                written to row lens[i] of the sequence (its page must be in the table) and takes part as the page holds it; lens is
+ *                not changed (several layers share it)
+ *   lens         DEVICE int32 [n_seqs]
+ *   out          DEVICE [n_seqs][Hq][d] dtype;  lse  DEVICE [n_seqs][Hq] fp32 or NULL: natural-log sum of exponentials
+ * A sequence without a row (lens[i] = 0, no new token) gets out = 0 and lse = -inf.  Bit-reproducible for equal lens. */
+int kvc_pool_decode(kvc_pool* pool, const void* q, long long q_stride, const void* k_new, const void* v_new,
+                    long long kv_stride, const int* table, int table_stride, const int* lens, int n_seqs, void* blob,
+                    void* workspace, void* out, float* lse, void* stream);
+
+/* Whole prompts of different lengths, packed one after the other.  The plan of a batch is made once on the host and serves all layers:
+ * kvc_pool_plan fills *plan and, if items is not NULL, items (HOST, plan->item_bytes bytes), which the caller copies to the device.
+ * lens: HOST [n_seqs], each >= 0 (a prompt of no tokens has no rows). */
+typedef struct {
+  int n_seqs;
+  long long n_tokens;  /* rows of q, k, v and out             */
+  int n_items;         /* pieces of work                       */
+  int row_tiles;       /* row tiles per piece (1 or 2), or rows per piece on the CUDA cores */
+  size_t item_bytes;   /* bytes of the items                   */
+} kvc_prompt_plan;
+int kvc_pool_plan(kvc_pool* pool, const int* lens, int n_seqs, kvc_prompt_plan* plan, void* items);
+
+/* Causal attention inside every prompt: row t of a prompt attends to its rows <= t.
+ *   q    DEVICE [n_tokens], rows of Hq x d at q_stride ELEMENTS;  k, v rows of Hkv x d at kv_stride
+ *   items  DEVICE copy of the plan's items;  out DEVICE [n_tokens][Hq][d];  lse DEVICE [n_tokens][Hq] fp32 or NULL
+ * Prompts do not see each other, whatever they hold; the values of one prompt have to be finite. */
+int kvc_pool_prompt(kvc_pool* pool, const void* q, long long q_stride, const void* k, const void* v, long long kv_stride,
+                    const kvc_prompt_plan* plan, const void* items, void* workspace, void* out, float* lse, void* stream);
+
+/* Synchronises `stream` and returns the workspace's status word: KVC_OK; KVC_EINVAL if a call since kvc_pool_workspace_init met a slot,
+ * page or length it had to leave out; KVC_ETIMEOUT if a bounded wait inside a kernel gave up. */
+int kvc_pool_status(kvc_pool* pool, void* workspace, void* stream);
+
+/* Kernel launches so far, and the text of the most recent error (never NULL). */
+long long kvc_pool_launch_count(const kvc_pool* pool);
+const char* kvc_pool_last_error(const kvc_pool* pool);
+
 #ifdef __cplusplus
 }
 #endif

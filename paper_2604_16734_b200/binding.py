@@ -17,6 +17,7 @@ from . import build as _build
 KVC_OK, KVC_EINVAL, KVC_ESTATE, KVC_ECUDA, KVC_ETIMEOUT = 0, -1, -2, -3, -4
 KVC_F32, KVC_BF16 = 0, 1
 KVC_SCORE_ATTN, KVC_SCORE_KEYDIFF = 0, 1
+KVC_PAGES_PLAIN, KVC_PAGES_INT8 = 0, 1
 KVC_FLAG_CUDA_CORES = 1
 KVC_FLAG_ASYNC_COMPRESS = 16
 
@@ -27,6 +28,8 @@ EXPORTS = [
     "kvc_join", "kvc_cache_view", "kvc_attention_shape", "kvc_workspace_view", "kvc_move_counts", "kvc_status", "kvc_kv_bytes", "kvc_profile_enable",
     "kvc_profile_read", "kvc_launch_count", "kvc_last_error", "kvc_set_wait_limit", "kvc_selftest_wait_timeout",
     "kvc_profile_device", "kvc_profile_device_read",
+    "kvc_pool_create", "kvc_pool_destroy", "kvc_pool_nbytes", "kvc_pool_workspace_init", "kvc_pool_write", "kvc_pool_read",
+    "kvc_pool_decode", "kvc_pool_plan", "kvc_pool_prompt", "kvc_pool_status", "kvc_pool_launch_count", "kvc_pool_last_error",
 ]
 
 
@@ -41,6 +44,18 @@ class KvcView(ctypes.Structure):
     _fields_ = [("k", ctypes.c_void_p), ("v", ctypes.c_void_p), ("pos", ctypes.c_void_p),
                 ("len", ctypes.c_int), ("cap", ctypes.c_int), ("n_kv_heads", ctypes.c_int),
                 ("head_dim", ctypes.c_int), ("dtype", ctypes.c_int)]
+
+
+class KvcPoolConfig(ctypes.Structure):
+    _fields_ = [("n_q_heads", ctypes.c_int), ("n_kv_heads", ctypes.c_int), ("head_dim", ctypes.c_int),
+                ("dtype", ctypes.c_int), ("page_format", ctypes.c_int), ("page_size", ctypes.c_int),
+                ("n_pages", ctypes.c_int), ("max_seqs", ctypes.c_int), ("softmax_scale", ctypes.c_float),
+                ("device", ctypes.c_int), ("flags", ctypes.c_uint)]
+
+
+class KvcPromptPlan(ctypes.Structure):
+    _fields_ = [("n_seqs", ctypes.c_int), ("n_tokens", ctypes.c_longlong), ("n_items", ctypes.c_int),
+                ("row_tiles", ctypes.c_int), ("item_bytes", ctypes.c_size_t)]
 
 
 def lib_path() -> str:
@@ -79,12 +94,22 @@ def load_library() -> ctypes.CDLL:
     lib.kvc_profile_read.argtypes = [vp, ctypes.POINTER(ctypes.c_double), ctypes.POINTER(ll)]
     lib.kvc_profile_device.argtypes = [vp, vp, ll, vp]
     lib.kvc_profile_device_read.argtypes = [vp, vp, ctypes.POINTER(ctypes.c_double), ctypes.POINTER(ll), ctypes.POINTER(ctypes.c_double)]
-    lib.kvc_launch_count.argtypes = [vp]
-    lib.kvc_launch_count.restype = ll
-    lib.kvc_last_error.argtypes = [vp]
-    lib.kvc_last_error.restype = ctypes.c_char_p
+    lib.kvc_pool_create.argtypes = [ctypes.POINTER(KvcPoolConfig), ctypes.POINTER(vp)]
+    lib.kvc_pool_destroy.argtypes = [vp]
+    lib.kvc_pool_nbytes.argtypes = [vp, psz, psz]
+    lib.kvc_pool_workspace_init.argtypes = [vp, vp, vp]
+    lib.kvc_pool_write.argtypes = [vp, vp, vp, ll, ll, vp, ll, vp, vp, vp]
+    lib.kvc_pool_read.argtypes = [vp, vp, vp, ll, vp, vp, ll, ll, vp, vp]
+    lib.kvc_pool_decode.argtypes = [vp, vp, ll, vp, vp, ll, vp, i, vp, i, vp, vp, vp, vp, vp]
+    lib.kvc_pool_plan.argtypes = [vp, vp, i, ctypes.POINTER(KvcPromptPlan), vp]
+    lib.kvc_pool_prompt.argtypes = [vp, vp, ll, vp, vp, ll, ctypes.POINTER(KvcPromptPlan), vp, vp, vp, vp, vp]
+    lib.kvc_pool_status.argtypes = [vp, vp, vp]
+    for name in ("kvc_launch_count", "kvc_pool_launch_count"):
+        getattr(lib, name).argtypes, getattr(lib, name).restype = [vp], ll
+    for name in ("kvc_last_error", "kvc_pool_last_error"):
+        getattr(lib, name).argtypes, getattr(lib, name).restype = [vp], ctypes.c_char_p
     for name in EXPORTS:
-        if name not in ("kvc_launch_count", "kvc_last_error"):
+        if not name.endswith(("launch_count", "last_error")):
             getattr(lib, name).restype = i
     return lib
 

@@ -9,8 +9,8 @@ import sys
 HERE = os.path.dirname(os.path.abspath(__file__))
 CSRC = os.path.join(HERE, "csrc")
 LIB = os.path.join(HERE, "libkvc.so")
-SOURCES = ["kvc_api.cu"]
-HEADERS = ["geom.cuh", "ptx.cuh", "kernels_cc.cuh", "kernels_tc.cuh", "compress.cuh"]
+SOURCES = ["kvc_api.cu", "pool_api.cu"]
+HEADERS = ["geom.cuh", "ptx.cuh", "kernels_cc.cuh", "kernels_tc.cuh", "compress.cuh", "pool.cuh"]
 
 
 def _stale() -> bool:
@@ -34,7 +34,7 @@ def build(force: bool = False, verbose: bool = False) -> str:
             return LIB                                    # no compiler here: use the library as shipped
         raise RuntimeError("libkvc.so is missing and nvcc was not found")
     cmd = [nvcc, "-gencode", "arch=compute_100a,code=sm_100a", "-lineinfo", "-O3", "-std=c++17",
-           "-shared", "-Xcompiler", "-fPIC", "-Xcompiler", "-fvisibility=default",
+           "--threads", str(len(SOURCES)), "-shared", "-Xcompiler", "-fPIC", "-Xcompiler", "-fvisibility=default",
            "-o", LIB + f".tmp{os.getpid()}"]
     if verbose:
         cmd += ["-Xptxas", "-v"]

@@ -1,0 +1,369 @@
+// Host side of the page pool's C ABI (see include/kvc.h): argument checks, plans, tensor maps and launches on the caller's
+// stream.  Allocates no device memory.
+#include "../../include/kvc.h"
+
+#include <cuda.h>
+#include <cuda_runtime.h>
+#include <math.h>
+#include <stdarg.h>
+#include <stdint.h>
+#include <stdio.h>
+#include <string.h>
+
+#include <algorithm>
+#include <new>
+
+#include "geom.cuh"
+#include "kernels_cc.cuh"
+#include "kernels_tc.cuh"
+#include "pool.cuh"
+
+typedef CUresult (*EncodeTiledFn)(CUtensorMap*, CUtensorMapDataType, cuuint32_t, void*, const cuuint64_t*,
+                                  const cuuint64_t*, const cuuint32_t*, const cuuint32_t*, CUtensorMapInterleave,
+                                  CUtensorMapSwizzle, CUtensorMapL2promotion, CUtensorMapFloatOOBfill);
+
+struct kvc_pool {
+  uint32_t magic;
+  kvc_pool_config cfg;
+  kvc::PoolGeom geom;
+  float scale;
+  size_t elem, blob_bytes, ws_bytes, ws_clear;
+  long long launches;
+  EncodeTiledFn encode;
+  char err[512];
+};
+
+static const uint32_t kPoolMagic = 0x6b76706cu;   // "kvpl"
+static const int kMaxDevices = 64;
+
+static size_t align_up(size_t x, size_t a) { return (x + a - 1) / a * a; }
+static bool aligned16(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 15) == 0; }
+static bool live(const kvc_pool* c) { return c && c->magic == kPoolMagic; }
+
+static int fail(kvc_pool* c, int code, const char* fmt, ...) {
+  va_list ap;
+  va_start(ap, fmt);
+  vsnprintf(c->err, sizeof(c->err), fmt, ap);
+  va_end(ap);
+  return code;
+}
+static int check_cuda(kvc_pool* c, cudaError_t e, const char* what) {
+  return e == cudaSuccess ? KVC_OK : fail(c, KVC_ECUDA, "%s: %s", what, cudaGetErrorString(e));
+}
+static int check_device(kvc_pool* c) {
+  int dev = -1;
+  if (cudaGetDevice(&dev) != cudaSuccess || dev != c->cfg.device)
+    return fail(c, KVC_ESTATE, "current CUDA device %d is not the pool's device %d", dev, c->cfg.device);
+  return KVC_OK;
+}
+// Strides of rows in elements: a multiple of 16 bytes, no shorter than the row.
+static bool stride_ok(const kvc_pool* c, long long stride, long long row) {
+  return stride >= row && stride <= (1ll << 40) && stride * (long long)c->elem % 16 == 0;
+}
+
+extern "C" int kvc_pool_create(const kvc_pool_config* cfg, kvc_pool** out) {
+  if (!out) return KVC_EINVAL;
+  *out = nullptr;
+  if (!cfg) return KVC_EINVAL;
+  if (cfg->n_kv_heads < 1 || cfg->n_q_heads < 1 || cfg->n_q_heads % cfg->n_kv_heads != 0) return KVC_EINVAL;
+  if (cfg->n_q_heads / cfg->n_kv_heads > 128 || cfg->n_q_heads > 65535) return KVC_EINVAL;
+  if (cfg->head_dim != 64 && cfg->head_dim != 128) return KVC_EINVAL;
+  if (cfg->dtype != KVC_F32 && cfg->dtype != KVC_BF16) return KVC_EINVAL;
+  if (cfg->page_format != KVC_PAGES_PLAIN && cfg->page_format != KVC_PAGES_INT8) return KVC_EINVAL;
+  int ps_log2 = 4;
+  while (ps_log2 <= 8 && (1 << ps_log2) != cfg->page_size) ++ps_log2;
+  if (ps_log2 > 8) return KVC_EINVAL;
+  if (cfg->n_pages < 1 || cfg->max_seqs < 1 || cfg->max_seqs > 65535) return KVC_EINVAL;
+  if (!(cfg->softmax_scale >= 0.f) || isinf(cfg->softmax_scale)) return KVC_EINVAL;
+  if (cfg->device < 0 || cfg->device >= kMaxDevices || cfg->flags) return KVC_EINVAL;
+  const double bytes = 2.0 * cfg->n_pages * cfg->n_kv_heads * cfg->page_size * cfg->head_dim * 4;
+  if (bytes > (double)(1ll << 46)) return KVC_EINVAL;
+
+  kvc_pool* c = new (std::nothrow) kvc_pool();
+  if (!c) return KVC_EINVAL;
+  c->magic = kPoolMagic;
+  c->cfg = *cfg;
+  c->elem = cfg->dtype == KVC_F32 ? 4 : 2;
+  c->scale = cfg->softmax_scale > 0.f ? cfg->softmax_scale : 1.0f / sqrtf((float)cfg->head_dim);
+  const bool i8 = cfg->page_format == KVC_PAGES_INT8;
+  const size_t rows = (size_t)cfg->n_pages * cfg->n_kv_heads * cfg->page_size;
+  const size_t part = rows * cfg->head_dim * (i8 ? 1 : c->elem), scales = i8 ? align_up(rows * 4, 256) : 0;
+  kvc::PoolGeom& g = c->geom;
+  g.Hq = cfg->n_q_heads; g.Hkv = cfg->n_kv_heads; g.G = g.Hq / g.Hkv; g.n_pages = cfg->n_pages; g.ps_log2 = ps_log2;
+  g.scale_log2 = c->scale * 1.4426950408889634f;
+  g.v_off = (long long)part; g.ks_off = (long long)(2 * part); g.vs_off = (long long)(2 * part + scales);
+  c->blob_bytes = 2 * part + 2 * scales;
+  c->ws_clear = kvc::kWsHeaderBytes;
+  c->ws_bytes = c->ws_clear;
+  c->launches = 0;
+  c->encode = nullptr;
+  c->err[0] = 0;
+  *out = c;
+  return KVC_OK;
+}
+
+extern "C" int kvc_pool_destroy(kvc_pool* c) {
+  if (!live(c)) return KVC_ESTATE;
+  c->magic = 0;
+  delete c;
+  return KVC_OK;
+}
+
+extern "C" const char* kvc_pool_last_error(const kvc_pool* c) { return live(c) ? c->err : "invalid pool"; }
+extern "C" long long kvc_pool_launch_count(const kvc_pool* c) { return live(c) ? c->launches : -1; }
+
+extern "C" int kvc_pool_nbytes(const kvc_pool* c, size_t* per_layer, size_t* workspace) {
+  if (!live(c)) return KVC_ESTATE;
+  if (per_layer) *per_layer = c->blob_bytes;
+  if (workspace) *workspace = c->ws_bytes;
+  return KVC_OK;
+}
+
+extern "C" int kvc_pool_workspace_init(kvc_pool* c, void* workspace, void* stream) {
+  if (!live(c)) return KVC_ESTATE;
+  if (!workspace || !aligned16(workspace)) return fail(c, KVC_EINVAL, "workspace pointer null or misaligned");
+  return check_cuda(c, cudaMemsetAsync(workspace, 0, c->ws_clear, (cudaStream_t)stream), "cudaMemsetAsync");
+}
+
+extern "C" int kvc_pool_status(kvc_pool* c, void* workspace, void* stream) {
+  if (!live(c)) return KVC_ESTATE;
+  if (!workspace) return fail(c, KVC_EINVAL, "null pointer argument");
+  int word = 0;
+  if (int rc = check_cuda(c, cudaMemcpyAsync(&word, workspace, sizeof(int), cudaMemcpyDeviceToHost, (cudaStream_t)stream), "cudaMemcpyAsync")) return rc;
+  if (int rc = check_cuda(c, cudaStreamSynchronize((cudaStream_t)stream), "cudaStreamSynchronize")) return rc;
+  if (word == KVC_EINVAL) return fail(c, KVC_EINVAL, "a slot, page or length lay outside the pool or the table and was left out");
+  if (word != 0) return fail(c, word == KVC_ETIMEOUT ? KVC_ETIMEOUT : KVC_ECUDA, "device status word %d", word);
+  return KVC_OK;
+}
+
+// What kvc_pool_write and kvc_pool_read check alike.
+static int check_rows(kvc_pool* c, const void* k, const void* v, long long ts, long long hs, const void* slots, long long n,
+                      const void* blob, const void* ws) {
+  const kvc_pool_config& cf = c->cfg;
+  if (n < 0 || n * cf.n_kv_heads > 0x7fffffffll) return fail(c, KVC_EINVAL, "n = %lld rows of %d kv-heads outside [0, 2^31)", n, cf.n_kv_heads);
+  if (n > 0 && (!k || !v || !slots)) return fail(c, KVC_EINVAL, "null pointer argument");
+  if (!blob || !ws) return fail(c, KVC_EINVAL, "null pointer argument");
+  if (!aligned16(k) || !aligned16(v) || !aligned16(blob) || !aligned16(ws) || (reinterpret_cast<uintptr_t>(slots) & 7))
+    return fail(c, KVC_EINVAL, "pointers must be 16-byte aligned (slots: 8)");
+  if (!stride_ok(c, ts, cf.head_dim) || !stride_ok(c, hs, cf.head_dim))
+    return fail(c, KVC_EINVAL, "strides %lld, %lld: multiples of 16 bytes, at least head_dim", ts, hs);
+  return check_device(c);
+}
+
+template <typename F>
+static cudaError_t by_shape(const kvc_pool* c, F f) {       // f(T, D, I8) as tags
+  const bool d128 = c->cfg.head_dim == 128, i8 = c->cfg.page_format == KVC_PAGES_INT8;
+  auto with_type = [&](auto t) {
+    if (d128) return i8 ? f(t, std::integral_constant<int, 128>(), std::true_type()) : f(t, std::integral_constant<int, 128>(), std::false_type());
+    return i8 ? f(t, std::integral_constant<int, 64>(), std::true_type()) : f(t, std::integral_constant<int, 64>(), std::false_type());
+  };
+  return c->cfg.dtype == KVC_F32 ? with_type(float()) : with_type(__nv_bfloat16());
+}
+
+extern "C" int kvc_pool_write(kvc_pool* c, const void* k, const void* v, long long token_stride, long long head_stride,
+                              const long long* slots, long long n, void* blob, void* workspace, void* stream) {
+  if (!live(c)) return KVC_ESTATE;
+  if (int rc = check_rows(c, k, v, token_stride, head_stride, slots, n, blob, workspace)) return rc;
+  if (n == 0) return KVC_OK;
+  const unsigned rows = (unsigned)(n * c->cfg.n_kv_heads);
+  const cudaError_t e = by_shape(c, [&](auto t, auto d, auto i8) {
+    using T = decltype(t);
+    constexpr int D = decltype(d)::value, per = kvc::pool_rows_per_block<T, D>();
+    kvc::pool_write_kernel<T, D, decltype(i8)::value><<<(rows + per - 1) / per, kvc::kPoolThreads, 0, (cudaStream_t)stream>>>(
+        (const T*)k, (const T*)v, token_stride, head_stride, slots, rows, (char*)blob, (char*)workspace, c->geom);
+    return cudaGetLastError();
+  });
+  c->launches++;
+  return check_cuda(c, e, "write launch");
+}
+
+extern "C" int kvc_pool_read(kvc_pool* c, const void* blob, const long long* slots, long long n, void* k, void* v,
+                             long long token_stride, long long head_stride, void* workspace, void* stream) {
+  if (!live(c)) return KVC_ESTATE;
+  if (int rc = check_rows(c, k, v, token_stride, head_stride, slots, n, blob, workspace)) return rc;
+  if (n == 0) return KVC_OK;
+  const unsigned rows = (unsigned)(n * c->cfg.n_kv_heads);
+  const cudaError_t e = by_shape(c, [&](auto t, auto d, auto i8) {
+    using T = decltype(t);
+    constexpr int D = decltype(d)::value, per = kvc::pool_rows_per_block<T, D>();
+    kvc::pool_read_kernel<T, D, decltype(i8)::value><<<(rows + per - 1) / per, kvc::kPoolThreads, 0, (cudaStream_t)stream>>>(
+        (const char*)blob, slots, rows, (T*)k, (T*)v, token_stride, head_stride, (char*)workspace, c->geom);
+    return cudaGetLastError();
+  });
+  c->launches++;
+  return check_cuda(c, e, "read launch");
+}
+
+extern "C" int kvc_pool_decode(kvc_pool* c, const void* q, long long q_stride, const void* k_new, const void* v_new,
+                               long long kv_stride, const int* table, int table_stride, const int* lens, int n_seqs, void* blob,
+                               void* workspace, void* out, float* lse, void* stream) {
+  if (!live(c)) return KVC_ESTATE;
+  const kvc_pool_config& cf = c->cfg;
+  if (n_seqs < 0 || n_seqs > cf.max_seqs) return fail(c, KVC_EINVAL, "n_seqs = %d outside [0, max_seqs = %d]", n_seqs, cf.max_seqs);
+  if (!blob || !workspace || (n_seqs > 0 && (!q || !table || !lens || !out))) return fail(c, KVC_EINVAL, "null pointer argument");
+  if (!k_new != !v_new) return fail(c, KVC_EINVAL, "k_new and v_new go together");
+  if (!aligned16(q) || !aligned16(k_new) || !aligned16(v_new) || !aligned16(blob) || !aligned16(workspace) || !aligned16(out))
+    return fail(c, KVC_EINVAL, "pointers must be 16-byte aligned");
+  if ((reinterpret_cast<uintptr_t>(table) | reinterpret_cast<uintptr_t>(lens) | reinterpret_cast<uintptr_t>(lse)) & 3)
+    return fail(c, KVC_EINVAL, "table, lens and lse must be 4-byte aligned");
+  if (table_stride < 0 || (k_new && table_stride < 1 && n_seqs > 0)) return fail(c, KVC_EINVAL, "table_stride = %d", table_stride);
+  if (((long long)table_stride << c->geom.ps_log2) > 0x7fffffffll) return fail(c, KVC_EINVAL, "table_stride = %d pages hold 2^31 tokens or more", table_stride);
+  if (!stride_ok(c, q_stride, (long long)cf.n_q_heads * cf.head_dim)) return fail(c, KVC_EINVAL, "q_stride = %lld", q_stride);
+  if (k_new && !stride_ok(c, kv_stride, (long long)cf.n_kv_heads * cf.head_dim)) return fail(c, KVC_EINVAL, "kv_stride = %lld", kv_stride);
+  if (int rc = check_device(c)) return rc;
+  if (n_seqs == 0) return KVC_OK;
+  const cudaError_t e = by_shape(c, [&](auto t, auto d, auto i8) {
+    using T = decltype(t);
+    constexpr int D = decltype(d)::value;
+    kvc::pool_decode_kernel<T, D, decltype(i8)::value><<<dim3(n_seqs, cf.n_kv_heads, (c->geom.G + 7) / 8), kvc::kDecodeWarps * 32, 0, (cudaStream_t)stream>>>(
+        (const T*)q, q_stride, (const T*)k_new, (const T*)v_new, kv_stride, table, table_stride, lens, (char*)blob, (char*)workspace, (T*)out, lse, c->geom);
+    return cudaGetLastError();
+  });
+  c->launches++;
+  return check_cuda(c, e, "decode launch");
+}
+
+// ------------------------------------------------------------------------------------------------ prompts
+// Pieces of work: {first token of the prompt, tokens of the prompt, first row tile, row tiles}, longest first.  A row tile is
+// 128 / G tokens on the tensor cores (bf16), BM rows of (token, head) on the CUDA cores (fp32).
+struct PromptItem { int first, len, tile, tiles; };
+
+static const int kPromptRowsCc = 32;
+
+static int plan_row_tiles(const kvc_pool* c, long long tiles) {
+  if (c->cfg.dtype == KVC_F32) return kPromptRowsCc;
+  return tiles * c->cfg.n_kv_heads > 2 * kvc::kNumSMs ? 2 : 1;
+}
+
+extern "C" int kvc_pool_plan(kvc_pool* c, const int* lens, int n_seqs, kvc_prompt_plan* plan, void* items) {
+  if (!live(c)) return KVC_ESTATE;
+  if (!plan || n_seqs < 0 || (n_seqs > 0 && !lens)) return fail(c, KVC_EINVAL, "null pointer argument or n_seqs = %d", n_seqs);
+  const bool f32 = c->cfg.dtype == KVC_F32;
+  const int G = c->geom.G, TOK = f32 ? 0 : 128 / G;
+  long long tokens = 0, tiles = 0;
+  for (int i = 0; i < n_seqs; ++i) {
+    if (lens[i] < 0) return fail(c, KVC_EINVAL, "lens[%d] = %d", i, lens[i]);
+    tokens += lens[i];
+    tiles += f32 ? ((long long)lens[i] * G + kPromptRowsCc - 1) / kPromptRowsCc : (lens[i] + TOK - 1) / TOK;
+  }
+  if (tokens * c->cfg.n_q_heads > 0x7fffffffll) return fail(c, KVC_EINVAL, "%lld tokens of %d query heads: 2^31 rows or more", tokens, c->cfg.n_q_heads);
+  const int R = plan_row_tiles(c, tiles);
+  long long n_items = 0;
+  for (int i = 0; i < n_seqs; ++i) {
+    const long long t = f32 ? ((long long)lens[i] * G + R - 1) / R : (lens[i] + TOK - 1) / TOK;
+    n_items += f32 || R == 1 ? t : (t + 1) / 2;
+  }
+  if (n_items > 0x7fffffffll) return fail(c, KVC_EINVAL, "%lld pieces of work", n_items);
+  plan->n_seqs = n_seqs;
+  plan->n_tokens = tokens;
+  plan->n_items = (int)n_items;
+  plan->row_tiles = R;
+  plan->item_bytes = sizeof(PromptItem) * (size_t)n_items;
+  if (!items) return KVC_OK;
+  PromptItem* it = (PromptItem*)items;
+  long long first = 0, n = 0;
+  for (int i = 0; i < n_seqs; ++i) {
+    const int t = f32 ? (int)(((long long)lens[i] * G + R - 1) / R) : (lens[i] + TOK - 1) / TOK;
+    const int step = f32 ? 1 : R;
+    for (int k = 0; k < t; k += step) it[n++] = {(int)first, lens[i], k, std::min(step, t - k)};
+    first += lens[i];
+  }
+  // longest first: a piece sees the keys up to its last token (ties keep their order, so a plan is the same every time)
+  auto cost = [&](const PromptItem& x) {
+    const long long last = f32 ? std::min<long long>(x.len, ((long long)(x.tile + 1) * R + G - 1) / G) : std::min<long long>(x.len, (long long)(x.tile + x.tiles) * TOK);
+    return (last + 127) / 128 * (f32 ? 1 : 1 + x.tiles);
+  };
+  std::stable_sort(it, it + n, [&](const PromptItem& a, const PromptItem& b) { return cost(a) > cost(b); });
+  return KVC_OK;
+}
+
+static int make_map(kvc_pool* c, CUtensorMap* m, const void* base, int d, int heads, long long tokens, long long stride, int box_heads, int box_tokens) {
+  const cuuint64_t gd[4] = {(cuuint64_t)d, (cuuint64_t)heads, (cuuint64_t)tokens, 1};
+  const cuuint64_t gs[3] = {(cuuint64_t)d * 2, (cuuint64_t)stride * 2, (cuuint64_t)stride * 2 * tokens};
+  const cuuint32_t bx[4] = {64, (cuuint32_t)box_heads, (cuuint32_t)box_tokens, 1};
+  const cuuint32_t es[4] = {1, 1, 1, 1};
+  const CUresult r = c->encode(m, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 4, const_cast<void*>(base), gd, gs, bx, es, CU_TENSOR_MAP_INTERLEAVE_NONE,
+                               CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_128B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
+  if (r != CUDA_SUCCESS) return fail(c, KVC_ECUDA, "cuTensorMapEncodeTiled failed (%d): %d heads, %lld tokens, stride %lld", (int)r, heads, tokens, stride);
+  return KVC_OK;
+}
+
+template <typename Kernel>
+static cudaError_t opt_in_smem(Kernel kernel, int bytes, bool* done_per_device, int dev) {
+  if (done_per_device[dev]) return cudaSuccess;
+  const cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, bytes);
+  if (e == cudaSuccess) done_per_device[dev] = true;
+  return e;
+}
+
+template <int D, int R>
+static cudaError_t launch_prompt_tc(const kvc_pool* c, const CUtensorMap (&m)[4], const kvc_prompt_plan* plan, const void* items,
+                                    void* ws, void* out, const kvc::Geom& g, cudaStream_t st) {
+  const int smem = (R + kvc::attn_stages<R>()) * (D / 64) * kvc::kSubTileBytes + 1024;
+  static bool attr_set[kMaxDevices] = {};
+  if (cudaError_t e = opt_in_smem(kvc::attn_tc_kernel<D, R, true>, smem, attr_set, c->cfg.device)) return e;
+  kvc::attn_tc_kernel<D, R, true><<<dim3(plan->n_items, g.Hkv), kvc::kAttnThreads, smem, st>>>(
+      m[0], m[1], m[2], m[1], m[2], m[3], (char*)const_cast<void*>(items), (__nv_bfloat16*)out, (char*)ws, g, 1, 0);
+  return cudaGetLastError();
+}
+
+template <int D>
+static cudaError_t launch_prompt_cc(const kvc_pool* c, const void* q, const void* k, const void* v, const kvc_prompt_plan* plan,
+                                    const void* items, void* ws, void* out, const kvc::Geom& g, cudaStream_t st) {
+  using L = kvc::AttnCc<D, kPromptRowsCc>;
+  static bool attr_set[kMaxDevices] = {};
+  if (cudaError_t e = opt_in_smem(kvc::attn_cc_kernel<float, D, kPromptRowsCc, true>, L::kBytes, attr_set, c->cfg.device)) return e;
+  kvc::attn_cc_kernel<float, D, kPromptRowsCc, true><<<dim3(plan->n_items, g.Hkv), kvc::kCcThreads, L::kBytes, st>>>(
+      (const float*)q, (const float*)k, (const float*)v, (char*)const_cast<void*>(items), (float*)out, (char*)ws, g, 1);
+  return cudaGetLastError();
+}
+
+extern "C" int kvc_pool_prompt(kvc_pool* c, const void* q, long long q_stride, const void* k, const void* v, long long kv_stride,
+                               const kvc_prompt_plan* plan, const void* items, void* workspace, void* out, float* lse, void* stream) {
+  if (!live(c)) return KVC_ESTATE;
+  const kvc_pool_config& cf = c->cfg;
+  if (!plan || !workspace) return fail(c, KVC_EINVAL, "null pointer argument");
+  const bool f32 = cf.dtype == KVC_F32;
+  if (plan->n_tokens < 0 || plan->n_items < 0 || plan->n_tokens * cf.n_q_heads > 0x7fffffffll || plan->item_bytes != sizeof(PromptItem) * (size_t)plan->n_items ||
+      (f32 ? plan->row_tiles != kPromptRowsCc : plan->row_tiles != 1 && plan->row_tiles != 2))
+    return fail(c, KVC_EINVAL, "the plan is not one of this pool's");
+  if (plan->n_tokens > 0 && (!q || !k || !v || !items || !out)) return fail(c, KVC_EINVAL, "null pointer argument");
+  if (!aligned16(q) || !aligned16(k) || !aligned16(v) || !aligned16(items) || !aligned16(workspace) || !aligned16(out) || (reinterpret_cast<uintptr_t>(lse) & 3))
+    return fail(c, KVC_EINVAL, "pointers must be 16-byte aligned (lse: 4)");
+  if (!stride_ok(c, q_stride, (long long)cf.n_q_heads * cf.head_dim) || !stride_ok(c, kv_stride, (long long)cf.n_kv_heads * cf.head_dim))
+    return fail(c, KVC_EINVAL, "strides %lld, %lld: multiples of 16 bytes, at least a token's heads", q_stride, kv_stride);
+  if (int rc = check_device(c)) return rc;
+  if (plan->n_tokens == 0) return KVC_OK;
+  kvc::Geom g;
+  memset(&g, 0, sizeof(g));
+  g.G = c->geom.G; g.Hq = cf.n_q_heads; g.Hkv = cf.n_kv_heads; g.d = cf.head_dim; g.nl = 1;
+  g.scale_log2 = c->geom.scale_log2;
+  g.q_ls = q_stride; g.kv_ls = kv_stride;
+  g.score_off = (long long)reinterpret_cast<intptr_t>(lse);
+  g.wait_limit_k = kvc::kDefaultWaitLimitK;
+  cudaError_t e;
+  if (f32) {
+    e = cf.head_dim == 128 ? launch_prompt_cc<128>(c, q, k, v, plan, items, workspace, out, g, (cudaStream_t)stream)
+                           : launch_prompt_cc<64>(c, q, k, v, plan, items, workspace, out, g, (cudaStream_t)stream);
+  } else {
+    if (!c->encode) {
+      void* fn = nullptr;
+      cudaDriverEntryPointQueryResult qres;
+      e = cudaGetDriverEntryPoint("cuTensorMapEncodeTiled", &fn, cudaEnableDefault, &qres);
+      if (e != cudaSuccess || qres != cudaDriverEntryPointSuccess || !fn)
+        return fail(c, KVC_ECUDA, "cuTensorMapEncodeTiled entry point unavailable: %s", cudaGetErrorString(e));
+      c->encode = (EncodeTiledFn)fn;
+    }
+    CUtensorMap m[4];
+    const int d = cf.head_dim, TOK = 128 / g.G;
+    if (int rc = make_map(c, &m[0], q, d, g.Hq, plan->n_tokens, q_stride, g.G, TOK)) return rc;
+    if (int rc = make_map(c, &m[1], k, d, g.Hkv, plan->n_tokens, kv_stride, 1, 128)) return rc;
+    if (int rc = make_map(c, &m[2], v, d, g.Hkv, plan->n_tokens, kv_stride, 1, 128)) return rc;
+    if (int rc = make_map(c, &m[3], out, d, g.Hq, plan->n_tokens, (long long)g.Hq * d, g.G, TOK)) return rc;
+    auto run = [&](auto launcher) { return launcher(c, m, plan, items, workspace, out, g, (cudaStream_t)stream); };
+    if (d == 128) e = plan->row_tiles == 2 ? run(launch_prompt_tc<128, 2>) : run(launch_prompt_tc<128, 1>);
+    else e = plan->row_tiles == 2 ? run(launch_prompt_tc<64, 2>) : run(launch_prompt_tc<64, 1>);
+  }
+  c->launches++;
+  return check_cuda(c, e, "prompt launch");
+}

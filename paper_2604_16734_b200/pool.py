@@ -1,0 +1,247 @@
+"""Python side of the page pool (include/kvc.h, ``kvc_pool_*``): answering from retained caches.
+
+Argument marshalling only, as in ``binding``: every step runs in the CUDA library, PyTorch holds the memory and the
+streams, and there is no CPU fallback.
+
+    pool = Pool(32, 8, 128, torch.bfloat16, n_pages=4096, page_format="int8", n_layers=32, max_seqs=64)
+    pool.write(layer, K[:, :n].transpose(0, 1), V[:, :n].transpose(0, 1), slots)   # a retained cache (Kvc.cache_view)
+    plan = pool.plan([17, 250, 3])                                                 # three prompts, packed
+    out, lse = pool.prompt(q, k, v, plan)
+    out, lse = pool.decode(layer, q, table, lens, k, v)                            # one new token per sequence
+
+A *slot* is ``page * page_size + row``; ``table`` holds a row of pages per sequence, ``lens`` how many rows it has.  All calls are
+asynchronous on the current stream; what they find wrong on the device (a slot or page outside the pool, a length beyond the table)
+is left out and reported by ``status()``.
+"""
+from __future__ import annotations
+
+import ctypes
+import dataclasses
+from typing import Optional, Sequence, Tuple
+
+import torch
+
+from .binding import KVC_BF16, KVC_F32, KVC_OK, KVC_PAGES_INT8, KVC_PAGES_PLAIN, KvcError, KvcPoolConfig, KvcPromptPlan, _raw_stream, lib
+
+
+@dataclasses.dataclass
+class PromptPlan:
+    """How a batch of packed prompts is cut into pieces of work; made once per batch, used by every layer."""
+
+    plan: KvcPromptPlan
+    items: torch.Tensor
+
+    @property
+    def n_tokens(self) -> int:
+        return self.plan.n_tokens
+
+
+class Pool:
+    """A pool of key/value pages for many sequences, and attention over it.
+
+    ``page_format`` "plain" holds ``dtype``, "int8" 8-bit codes with a scale per (token, kv-head).  ``blob`` may be a
+    caller's own uint8 tensor [n_layers, Pool bytes per layer] instead of one allocated here.
+    """
+
+    def __init__(self, n_q_heads: int, n_kv_heads: int, head_dim: int, dtype: torch.dtype, n_pages: int, page_size: int = 64,
+                 page_format: str = "plain", n_layers: int = 1, max_seqs: int = 256, softmax_scale: float = 0.0, device: int = 0,
+                 blob: Optional[torch.Tensor] = None):
+        if not torch.cuda.is_available():
+            raise RuntimeError("kvc needs a CUDA device: there is no CPU implementation")
+        self._lib = lib()
+        self.dtype, self.device, self.head_dim = dtype, torch.device("cuda", device), head_dim
+        self.n_q_heads, self.n_kv_heads, self.page_size, self.n_pages = n_q_heads, n_kv_heads, page_size, n_pages
+        self.page_format = page_format
+        code = {torch.float32: KVC_F32, torch.bfloat16: KVC_BF16}[dtype]
+        pages = {"plain": KVC_PAGES_PLAIN, "int8": KVC_PAGES_INT8}[page_format]
+        cfg = KvcPoolConfig(n_q_heads, n_kv_heads, head_dim, code, pages, page_size, n_pages, max_seqs, softmax_scale, device, 0)
+        h = ctypes.c_void_p()
+        rc = self._lib.kvc_pool_create(ctypes.byref(cfg), ctypes.byref(h))
+        if rc != KVC_OK:
+            raise KvcError(rc, "kvc_pool_create rejected the configuration")
+        self._h = h
+        a, b = ctypes.c_size_t(), ctypes.c_size_t()
+        self._check(self._lib.kvc_pool_nbytes(self._h, ctypes.byref(a), ctypes.byref(b)))
+        self.blob_bytes, self.ws_bytes = a.value, b.value
+        if blob is not None and (blob.dtype != torch.uint8 or blob.dim() != 2 or blob.stride(1) != 1 or blob.shape[1] < self.blob_bytes
+                                 or blob.stride(0) % 256 and blob.shape[0] > 1 or blob.data_ptr() % 256 or blob.device != self.device):
+            raise ValueError(f"blob: a uint8 tensor [layers, {self.blob_bytes}] on {self.device}, rows at multiples of 256 bytes")
+        with torch.cuda.device(self.device):
+            # (zeros: a page that was never written holds numbers, whatever reads it)
+            self.blob = torch.zeros(n_layers, -(-self.blob_bytes // 256) * 256, dtype=torch.uint8, device=self.device) if blob is None else blob
+            self.workspace = torch.empty(self.ws_bytes, dtype=torch.uint8, device=self.device)
+            self.workspace_init()
+
+    # -- helpers ---------------------------------------------------------------------------------
+    def _stream(self) -> int:
+        return _raw_stream(self.device.index)
+
+    def _layer(self, layer: int) -> int:
+        if not 0 <= layer < self.blob.shape[0]:
+            raise IndexError(f"layer {layer} outside [0, {self.blob.shape[0]})")
+        return self.blob.data_ptr() + layer * self.blob.stride(0)
+
+    def _check(self, rc: int):
+        if rc != KVC_OK:
+            raise KvcError(rc, self._lib.kvc_pool_last_error(self._h).decode())
+
+    def close(self):
+        if getattr(self, "_h", None):
+            self._lib.kvc_pool_destroy(self._h)
+            self._h = None
+
+    def __del__(self):
+        try:
+            self.close()
+        except Exception:
+            pass
+
+    def _rows(self, name: str, t: torch.Tensor, n: int, heads: int) -> torch.Tensor:
+        """A tensor of rows [n][heads][d] of the pool's dtype; the strides of the first two dimensions are free."""
+        if t.shape != (n, heads, self.head_dim) or t.dtype != self.dtype or t.device != self.device or (t.stride(2) != 1 and t.numel()):
+            raise ValueError(f"{name}: {self.dtype} rows [{n}, {heads}, {self.head_dim}] on {self.device}, innermost contiguous; got "
+                             f"{t.dtype} {list(t.shape)} with strides {list(t.stride())} on {t.device}")
+        return t
+
+    def _token_rows(self, name: str, t: torch.Tensor, n: int, heads: int) -> int:
+        """The same with a token's heads side by side; the stride of a token's rows, in elements."""
+        self._rows(name, t, n, heads)
+        if heads > 1 and t.stride(1) != self.head_dim and t.numel():
+            raise ValueError(f"{name}: the heads of a token must be contiguous, strides {list(t.stride())}")
+        return max(t.stride(0), heads * self.head_dim) if n <= 1 else t.stride(0)
+
+    def _index(self, name: str, t: torch.Tensor, dtype: torch.dtype) -> int:
+        if t.dtype != dtype or t.device != self.device or not t.is_contiguous():
+            raise ValueError(f"{name}: a contiguous {dtype} tensor on {self.device}; got {t.dtype} on {t.device}")
+        return t.data_ptr()
+
+    def _pair_strides(self, k: torch.Tensor, v: torch.Tensor) -> Tuple[int, int]:
+        """Strides (token, kv-head) of two row tensors, which must agree; dimensions of one element may say anything."""
+        ts, hs = k.stride(0), k.stride(1)
+        if k.shape[0] > 1 and v.stride(0) != ts or k.shape[1] > 1 and v.stride(1) != hs:
+            raise ValueError(f"k and v must have the same strides; got {list(k.stride())} and {list(v.stride())}")
+        return (ts if k.shape[0] > 1 else self.head_dim), (hs if k.shape[1] > 1 else self.head_dim)
+
+    # -- pages -----------------------------------------------------------------------------------
+    def slots(self, pages: torch.Tensor, n: int, first: int = 0) -> torch.Tensor:
+        """int64 [n]: the slots of rows first .. first + n - 1 of a sequence whose pages (a row of a table) are given."""
+        at = torch.arange(first, first + n, device=pages.device)
+        return pages.long()[at // self.page_size] * self.page_size + at % self.page_size
+
+    def pages(self, layer: int) -> Tuple[torch.Tensor, ...]:
+        """(K, V) or (K codes, V codes, K scales, V scales) of a layer, aliasing the blob: [page][kv-head][row]([d])."""
+        held = (self.n_pages, self.n_kv_heads, self.page_size, self.head_dim)
+        rows = self.n_pages * self.n_kv_heads * self.page_size
+        blob = self.blob[layer]
+        if self.page_format == "plain":
+            size = rows * self.head_dim * self.dtype.itemsize
+            return tuple(blob[i * size:(i + 1) * size].view(self.dtype).view(held) for i in (0, 1))
+        size, up = rows * self.head_dim, -(-rows * 4 // 256) * 256
+        return tuple(blob[i * size:(i + 1) * size].view(torch.int8).view(held) for i in (0, 1)) + \
+            tuple(blob[2 * size + i * up:][:rows * 4].view(torch.float32).view(held[:3]) for i in (0, 1))
+
+    def write(self, layer: int, k: torch.Tensor, v: torch.Tensor, slots: torch.Tensor) -> None:
+        """Rows k, v [n][Hkv][d] (any strides of the first two dimensions, the same for both) into ``slots`` int64 [n]."""
+        n = slots.shape[0]
+        self._rows("k", k, n, self.n_kv_heads)
+        self._rows("v", v, n, self.n_kv_heads)
+        ts, hs = self._pair_strides(k, v)
+        self._check(self._lib.kvc_pool_write(self._h, k.data_ptr(), v.data_ptr(), ts, hs, self._index("slots", slots, torch.int64), n,
+                                             self._layer(layer), self.workspace.data_ptr(), self._stream()))
+
+    def read(self, layer: int, slots: torch.Tensor, k: Optional[torch.Tensor] = None,
+             v: Optional[torch.Tensor] = None) -> Tuple[torch.Tensor, torch.Tensor]:
+        """Slots back as rows [n][Hkv][d] of the pool's dtype, into k and v if given."""
+        n = slots.shape[0]
+        if (k is None) != (v is None):
+            raise ValueError("k and v go together")
+        if k is None:
+            k, v = torch.empty(2, n, self.n_kv_heads, self.head_dim, dtype=self.dtype, device=self.device)
+        self._rows("k", k, n, self.n_kv_heads)
+        self._rows("v", v, n, self.n_kv_heads)
+        ts, hs = self._pair_strides(k, v)
+        self._check(self._lib.kvc_pool_read(self._h, self._layer(layer), self._index("slots", slots, torch.int64), n, k.data_ptr(),
+                                            v.data_ptr(), ts, hs, self.workspace.data_ptr(), self._stream()))
+        return k, v
+
+    # -- attention -------------------------------------------------------------------------------
+    def _results(self, n: int, out: Optional[torch.Tensor], lse: Optional[torch.Tensor]) -> Tuple[torch.Tensor, torch.Tensor]:
+        if out is None:
+            out = torch.empty(n, self.n_q_heads, self.head_dim, dtype=self.dtype, device=self.device)
+        elif not self._rows("out", out, n, self.n_q_heads).is_contiguous():
+            raise ValueError("out must be contiguous")
+        if lse is None:
+            lse = torch.empty(n, self.n_q_heads, dtype=torch.float32, device=self.device)
+        else:
+            self._index("lse", lse, torch.float32)
+            if lse.shape != (n, self.n_q_heads):
+                raise ValueError(f"lse: [{n}, {self.n_q_heads}]; got {list(lse.shape)}")
+        return out, lse
+
+    def decode(self, layer: int, q: torch.Tensor, table: torch.Tensor, lens: torch.Tensor, k: Optional[torch.Tensor] = None,
+               v: Optional[torch.Tensor] = None, out: Optional[torch.Tensor] = None,
+               lse: Optional[torch.Tensor] = None) -> Tuple[torch.Tensor, torch.Tensor]:
+        """(out [n][Hq][d], lse [n][Hq]) of one new token per sequence: q [n][Hq][d], table int32 [n][pages], lens int32 [n].
+
+        With k, v [n][Hkv][d] the token's own row is written to row ``lens[i]`` of its sequence and takes part; ``lens`` stays as
+        it is (the caller adds one when all layers are done).
+        """
+        n = q.shape[0]
+        q_stride = self._token_rows("q", q, n, self.n_q_heads)
+        if table.dim() != 2 or table.shape[0] != n or lens.shape != (n,):
+            raise ValueError(f"table [{n}, pages] and lens [{n}]; got {list(table.shape)} and {list(lens.shape)}")
+        if (k is None) != (v is None):
+            raise ValueError("k and v go together")
+        kv_stride, kp, vp = 0, None, None
+        if k is not None:
+            kv_stride = self._token_rows("k", k, n, self.n_kv_heads)
+            if self._token_rows("v", v, n, self.n_kv_heads) != kv_stride:
+                raise ValueError(f"k and v must have the same strides; got {list(k.stride())} and {list(v.stride())}")
+            kp, vp = k.data_ptr(), v.data_ptr()
+        out, lse = self._results(n, out, lse)
+        rc = self._lib.kvc_pool_decode(self._h, q.data_ptr(), q_stride, kp, vp, kv_stride, self._index("table", table, torch.int32),
+                                       table.shape[1], self._index("lens", lens, torch.int32), n, self._layer(layer),
+                                       self.workspace.data_ptr(), out.data_ptr(), lse.data_ptr(), self._stream())
+        if rc:
+            self._check(rc)
+        return out, lse
+
+    def plan(self, lens: Sequence[int]) -> PromptPlan:
+        """The plan of prompts of these lengths (host numbers), packed in this order."""
+        lens = [int(x) for x in lens]
+        if any(not -2 ** 31 <= x < 2 ** 31 for x in lens):
+            raise ValueError("lengths are 32-bit numbers")
+        arr = (ctypes.c_int * len(lens))(*lens)
+        plan = KvcPromptPlan()
+        self._check(self._lib.kvc_pool_plan(self._h, arr, len(lens), ctypes.byref(plan), None))
+        items = torch.empty(plan.item_bytes, dtype=torch.uint8)
+        self._check(self._lib.kvc_pool_plan(self._h, arr, len(lens), ctypes.byref(plan), items.data_ptr() if plan.item_bytes else None))
+        return PromptPlan(plan, items.to(self.device))
+
+    def prompt(self, q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, plan: PromptPlan, out: Optional[torch.Tensor] = None,
+               lse: Optional[torch.Tensor] = None) -> Tuple[torch.Tensor, torch.Tensor]:
+        """(out [N][Hq][d], lse [N][Hq]) of packed prompts q [N][Hq][d], k, v [N][Hkv][d], causal inside each."""
+        n = plan.plan.n_tokens
+        q_stride = self._token_rows("q", q, n, self.n_q_heads)
+        kv_stride = self._token_rows("k", k, n, self.n_kv_heads)
+        if self._token_rows("v", v, n, self.n_kv_heads) != kv_stride:
+            raise ValueError(f"k and v must have the same strides; got {list(k.stride())} and {list(v.stride())}")
+        out, lse = self._results(n, out, lse)
+        rc = self._lib.kvc_pool_prompt(self._h, q.data_ptr(), q_stride, k.data_ptr(), v.data_ptr(), kv_stride, ctypes.byref(plan.plan),
+                                       plan.items.data_ptr(), self.workspace.data_ptr(), out.data_ptr(), lse.data_ptr(), self._stream())
+        if rc:
+            self._check(rc)
+        return out, lse
+
+    # -- state -----------------------------------------------------------------------------------
+    def workspace_init(self) -> None:
+        self._check(self._lib.kvc_pool_workspace_init(self._h, self.workspace.data_ptr(), self._stream()))
+
+    def status(self) -> int:
+        return self._lib.kvc_pool_status(self._h, self.workspace.data_ptr(), self._stream())
+
+    def launch_count(self) -> int:
+        return self._lib.kvc_pool_launch_count(self._h)
+
+    def last_error(self) -> str:
+        return self._lib.kvc_pool_last_error(self._h).decode()
