@@ -2,6 +2,7 @@
 // over its pages.
 #pragma once
 #include "geom.cuh"
+#include "kernels_cc.cuh"
 #include "ptx.cuh"
 
 namespace kvc {
@@ -11,7 +12,9 @@ struct PoolGeom {
   int Hq, Hkv, G, n_pages;
   int ps_log2;                     // page size = 1 << ps_log2
   float scale_log2;                // softmax scale times log2(e)
+  int min_tiles;                   // decode: fewest tiles of 16 keys that a CTA gets
   long long v_off, ks_off, vs_off; // byte offsets inside a blob of V, K scales, V scales (K is at 0)
+  long long joints_off;            // byte offset in the workspace of the pieces of segments that span CTAs
 };
 
 static constexpr int kPoolInvalid = -1;   // KVC_EINVAL in the status word: a slot, page or length had to be left out
@@ -186,100 +189,645 @@ __global__ void __launch_bounds__(kPoolThreads) pool_read_kernel(const char* __r
 }
 
 // ------------------------------------------------------------------------------------------------
-// One new token per sequence over its pages.  A CTA takes a (sequence, kv-head, eight of its query heads), its warps take keys in
-// turn with a running maximum, sum and output per head; a lane holds D / 32 channels.  grid (n_seqs, Hkv, ceil(G / 8)), block 128.
-static constexpr int kDecodeWarps = 4;
+// One new token per sequence over its pages.
+//
+// Mathematics: for every (sequence, kv-head) and its G query heads, s = scale * K q, o = V^T p / sum p with p = 2^(s - m) and a
+// running reference m.  Keys stand on the rows of the matrix instruction and query heads on its eight columns: S^T = K Q^T and
+// O^T = V^T P^T, so that up to eight heads cost one instruction where heads as rows would leave half of sixteen empty.
+// Bound: HBM, G FLOP per byte at bf16.  So pages go from global memory straight into the registers of the lane that feeds
+// them to the matrix instruction, 16 bytes per load: the order of a contraction is free, hence lane (r, c) = (lane / 4,
+// lane % 4) takes whole 16-byte pieces of a key's row, and the query's fragment is laid out the same way.  Values need
+// pairs of keys side by side (two bytes permutes per pair of words); eight lanes read a row's 128 bytes at once.
+// Neither shared memory nor a barrier is on the way, a tile's loads are issued while the one before is computed.
+//
+// Work: tiles of 16 keys of all (sequence, kv-head, head group) segments form one line, cut into equal ranges for the CTAs and
+// those for the warps, whatever the sequences' lengths (which only the device knows).  A warp that has a whole segment
+// writes its output; pieces are joined in shared memory, and pieces of a segment that spans CTAs in the workspace by the CTA that comes
+// last -- in the order of the pieces, so that results do not depend on who that is.
+//
+// 8 bits: codes become fp16 exactly (1024 + 128 + c, less 1152, as bit patterns); a key's scale multiplies its score, a value's scale goes
+// into its weight p * s, with a reference 2^m2 of its own in units of 2^m (the largest weight is near 2^7, so that fp16 has room below).
+// Queries are brought into fp16 by a power of two per head, in one part (bf16: exact for all but negligible channels) or two (fp32).
+// Probabilities are rounded to the type of the values' product: bf16 as in the attention of a block (2^-9 each, of the
+// size of the output's own rounding), fp16 2^-12, and fp32 in two parts.
+// fp32 pages: three products of TF32 parts (x = hi + lo: hi hi + hi lo + lo hi, 2^-21 and below), sums in fp32.
 
 template <typename T, int D, bool I8>
-__device__ __forceinline__ void key_values(const char* codes, const float* scales, long long row, int lane, float* x) {
-  constexpr int E = D / 32;
+struct DecodeShape {
+  static constexpr bool F32 = sizeof(T) == 4 && !I8;        // fp32 pages
+  static constexpr int NT = F32 ? 1 : 2;                    // most groups of eight query heads per segment
+  static constexpr int ROWB = D * (I8 ? 1 : (int)sizeof(T));
+  static constexpr int CK = ROWB / 64;                      // 16-byte pieces of a key's row per lane (of a quad)
+  static constexpr int VB = ROWB >= 128 ? 16 : 8;           // bytes of a value's row per lane (of eight) and piece
+  static constexpr int CV = ROWB / (8 * VB);
+  static constexpr int E = VB / (I8 ? 1 : (int)sizeof(T));  // channels in such a piece
+  static constexpr int MT = D / 16;                         // sixteen-channel blocks of the output
+  static constexpr int QP = I8 && sizeof(T) == 4 ? 2 : 1;   // parts of a query or probability
+  static constexpr int KS = F32 ? D / 8 : D / 16;           // steps of the contraction over channels
+};
+static constexpr int kDecodeWarps = 8, kDecodeThreads = kDecodeWarps * 32;
+static constexpr int kDecodeMaxCtas = kNumSMs * 2;
+static constexpr int kDecodeMaxSeqs = 4096;                 // the sequences' tile counts are kept in shared memory
+__host__ __device__ constexpr int decode_row(int D) { return D + 4; }    // floats of a head's row of a piece: O, m, l
+static constexpr int kDecodePieceFloats = 16 * (128 + 4);   // a piece in the workspace: up to 16 heads
+
+__device__ __forceinline__ uint4 ldg16(const void* p) {      // read once: not kept in L1
+  uint4 r;
+  asm volatile("ld.global.L1::no_allocate.v4.u32 {%0, %1, %2, %3}, [%4];" : "=r"(r.x), "=r"(r.y), "=r"(r.z), "=r"(r.w) : "l"(p) : "memory");
+  return r;
+}
+__device__ __forceinline__ uint2 ldg8(const void* p) {
+  uint2 r;
+  asm volatile("ld.global.L1::no_allocate.v2.u32 {%0, %1}, [%2];" : "=r"(r.x), "=r"(r.y) : "l"(p) : "memory");
+  return r;
+}
+__device__ __forceinline__ float ldg_f32(const float* p) {
+  float r;
+  asm volatile("ld.global.f32 %0, [%1];" : "=f"(r) : "l"(p) : "memory");
+  return r;
+}
+__device__ __forceinline__ void mma_bf16(float* d, const uint32_t* a, uint32_t b0, uint32_t b1) {
+  asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, {%0, %1, %2, %3};"
+               : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3]) : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
+}
+__device__ __forceinline__ void mma_f16(float* d, const uint32_t* a, uint32_t b0, uint32_t b1) {
+  asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, {%0, %1, %2, %3};"
+               : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3]) : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
+}
+__device__ __forceinline__ void mma_tf32(float* d, const uint32_t* a, uint32_t b0, uint32_t b1) {
+  asm volatile("mma.sync.aligned.m16n8k8.row.col.f32.tf32.tf32.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, {%0, %1, %2, %3};"
+               : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3]) : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
+}
+// x = hi + lo in TF32 (eleven bits; the instruction drops those behind).  Both are rounded, not cut: cut parts are all off towards
+// zero, which adds up over a dot product (log-sum-exp of scores around 600: off by 6e-4 instead of below 1e-4).
+__device__ __forceinline__ void split_tf32(uint32_t x, uint32_t& hi, uint32_t& lo) {
+  hi = (x + 0x1000u) & 0xffffe000u;
+  lo = __float_as_uint(__uint_as_float(x) - __uint_as_float(hi)) + 0x1000u;
+}
+__device__ __forceinline__ void mma_3tf32(float* d, const uint32_t* x, uint32_t b0, uint32_t b1) {
+  uint32_t hi[4], lo[4], bh0, bl0, bh1, bl1;
 #pragma unroll
-  for (int i = 0; i < E; ++i) {
-    const long long at = row * D + lane * E + i;
-    if constexpr (I8) x[i] = scales[row] * static_cast<float>(reinterpret_cast<const signed char*>(codes)[at]);
-    else x[i] = static_cast<float>(reinterpret_cast<const T*>(codes)[at]);
-  }
+  for (int i = 0; i < 4; ++i) split_tf32(x[i], hi[i], lo[i]);
+  split_tf32(b0, bh0, bl0);
+  split_tf32(b1, bh1, bl1);
+  mma_tf32(d, lo, bh0, bh1);
+  mma_tf32(d, hi, bl0, bl1);
+  mma_tf32(d, hi, bh0, bh1);
+}
+__device__ __forceinline__ uint32_t transpose8(uint32_t x) {   // an 8 x 8 matrix of 16-bit values over the warp
+  uint32_t r;
+  asm volatile("movmatrix.sync.aligned.m8n8.trans.b16 %0, %1;" : "=r"(r) : "r"(x));
+  return r;
+}
+__device__ __forceinline__ uint32_t pack_f16x2(float lo, float hi) {
+  uint32_t r;
+  asm("cvt.rn.f16x2.f32 %0, %1, %2;" : "=r"(r) : "f"(hi), "f"(lo));
+  return r;
+}
+__device__ __forceinline__ float f16_lo(uint32_t x) { float r; asm("{.reg .b16 l, h; mov.b32 {l, h}, %1; cvt.f32.f16 %0, l;}" : "=f"(r) : "r"(x)); return r; }
+__device__ __forceinline__ float f16_hi(uint32_t x) { float r; asm("{.reg .b16 l, h; mov.b32 {l, h}, %1; cvt.f32.f16 %0, h;}" : "=f"(r) : "r"(x)); return r; }
+// Two biased codes (c + 128) in bytes `sel` of x as fp16: 0x6400 + u is 1024 + u.
+template <uint32_t SEL> __device__ __forceinline__ uint32_t codes_f16(uint32_t x) {
+  uint32_t r;
+  asm("{.reg .b32 t; prmt.b32 t, %1, 0x64646464, %2; sub.rn.f16x2 %0, t, %3;}" : "=r"(r) : "r"(x), "n"(SEL), "r"(0x64806480u));
+  return r;
 }
 
-template <typename T, int D, bool I8>
-__global__ void __launch_bounds__(kDecodeWarps * 32) pool_decode_kernel(const T* __restrict__ q, long long q_stride,
-                                                                        const T* __restrict__ k_new, const T* __restrict__ v_new,
-                                                                        long long kv_stride, const int* __restrict__ table,
-                                                                        int table_stride, const int* __restrict__ lens,
-                                                                        char* blob, char* __restrict__ ws, T* __restrict__ out,
-                                                                        float* __restrict__ lse, PoolGeom p) {
-  constexpr int E = D / 32, LANES = D / Piece<T>::N;
-  __shared__ float sO[kDecodeWarps][8][D], sM[kDecodeWarps][8], sL[kDecodeWarps][8];
-  const int seq = blockIdx.x, g = blockIdx.y, h0 = blockIdx.z * 8, warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
-  const int heads = min(8, p.G - h0);
-  float* ks = reinterpret_cast<float*>(blob + p.ks_off);
-  float* vs = reinterpret_cast<float*>(blob + p.vs_off);
-  const int* pages = table + static_cast<long long>(seq) * table_stride;
-  long long len = lens[seq];
-  const long long room = (static_cast<long long>(table_stride) << p.ps_log2) - (k_new ? 1 : 0);
-  if (len < 0 || len > room) { if (threadIdx.x == 0) pool_refuse(ws); len = len < 0 ? 0 : room; }
-  auto row_of = [&](long long j) { return pool_row(p, (static_cast<long long>(pages[j >> p.ps_log2]) << p.ps_log2) + (j & ((1 << p.ps_log2) - 1)), g); };
-  if (k_new) {                                               // the token's own row, by every CTA that reads it (the same bytes)
-    const long long dst = row_of(len);
-    if (warp == 0) {
-      const int piece = lane % LANES;
-      const long long src = seq * kv_stride + static_cast<long long>(g) * D + piece * Piece<T>::N;
-      const long long to = lane < LANES ? dst : -1;
-      put_row<T, D, I8>(blob, ks, to, piece, *reinterpret_cast<const uint4*>(k_new + src));
-      put_row<T, D, I8>(blob + p.v_off, vs, to, piece, *reinterpret_cast<const uint4*>(v_new + src));
+// What a lane holds of the sixteen keys and values of a tile.
+template <typename T, int D, bool I8> struct TileRegs {
+  using S = DecodeShape<T, D, I8>;
+  uint4 k[2][S::CK];               // rows r and r + 8
+  uint4 v[4][S::CV];               // rows 2c, 2c + 1, 2c + 8, 2c + 9 (fp32: c, c + 4, c + 8, c + 12)
+  float ks[2], vs[2];              // scales of rows r and r + 8
+};
+
+template <typename T, int D, bool I8, int NT>
+struct Decoder {
+  using S = DecodeShape<T, D, I8>;
+  static constexpr int QR = S::KS * 2 * S::QP;
+  uint32_t qf[NT][QR];
+  float hf[NT][2];                 // 8 bits: 2^e * scale of heads 2c, 2c + 1
+  float acc[NT][S::MT][4], m[NT][2], m2[NT][2], l[NT][2];
+
+  static __device__ __forceinline__ int v_row(int c, int i) { return S::F32 ? c + 4 * i : 2 * c + (i & 1) + 8 * (i >> 1); }
+
+  // heads [0, heads) of the segment start at q
+  __device__ __forceinline__ void begin(const T* q, int heads, float scale_log2) {
+    const int lane = threadIdx.x & 31, r = lane >> 2, c = lane & 3;
+#pragma unroll
+    for (int n = 0; n < NT; ++n) {
+      const int h = n * 8 + r;
+      const bool there = h < heads;
+      if constexpr (!I8) {
+#pragma unroll
+        for (int j = 0; j < S::CK; ++j) {
+          const uint4 w = there ? *reinterpret_cast<const uint4*>(q + h * D + (c + 4 * j) * (16 / (int)sizeof(T))) : make_uint4(0, 0, 0, 0);
+          qf[n][4 * j] = w.x; qf[n][4 * j + 1] = w.y; qf[n][4 * j + 2] = w.z; qf[n][4 * j + 3] = w.w;
+        }
+      } else {
+        // channels 16 (c + 4 j) + 4 w + {0, 1 | 2, 3} in step 4 j + w
+        float x[S::KS][4], top = 0.f;
+#pragma unroll
+        for (int j = 0; j < S::CK; ++j)
+#pragma unroll
+          for (int i = 0; i < 16 / Piece<T>::N; ++i) {
+            const uint4 w = there ? *reinterpret_cast<const uint4*>(q + h * D + (c + 4 * j) * 16 + i * Piece<T>::N) : make_uint4(0, 0, 0, 0);
+            Piece<T>::values(w, &x[4 * j][0] + i * Piece<T>::N);
+          }
+#pragma unroll
+        for (int i = 0; i < S::KS * 4; ++i) top = fmaxf(top, fabsf((&x[0][0])[i]));
+        top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, 1));
+        top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, 2));
+        // the largest channel between 2^14 and 2^15; powers of two in two halves, as one may be out of range
+        const int e = top > 0.f && top < INFINITY ? ilogbf(top) - 14 : 0;
+        const float d0 = __uint_as_float((127u - e / 2) << 23), d1 = __uint_as_float((127u - (e - e / 2)) << 23);
+#pragma unroll
+        for (int k = 0; k < S::KS; ++k)
+#pragma unroll
+          for (int i = 0; i < 2; ++i) {
+            const float a = x[k][2 * i] * d0 * d1, b = x[k][2 * i + 1] * d0 * d1;
+            const uint32_t hi = pack_f16x2(a, b);
+            qf[n][2 * k + i] = hi;
+            if constexpr (S::QP == 2) qf[n][2 * S::KS + 2 * k + i] = pack_f16x2(a - f16_lo(hi), b - f16_hi(hi));
+          }
+        // the factor of heads 2c, 2c + 1 stands with the lanes of row r = head
+#pragma unroll
+        for (int i = 0; i < 2; ++i) {
+          const int eh = __shfl_sync(0xffffffffu, e, (2 * c + i) * 4);
+          hf[n][i] = ldexpf(scale_log2, eh);
+        }
+      }
+#pragma unroll
+      for (int i = 0; i < 2; ++i) { m[n][i] = -INFINITY; m2[n][i] = -INFINITY; l[n][i] = 0.f; if constexpr (!I8) hf[n][i] = scale_log2; }
+#pragma unroll
+      for (int t = 0; t < S::MT; ++t)
+#pragma unroll
+        for (int i = 0; i < 4; ++i) acc[n][t][i] = 0.f;
     }
-    ++len;
+  }
+
+  // row: first of the tile's sixteen rows in the pages (negative: none, the tile counts for nothing)
+  __device__ __forceinline__ void load_k(TileRegs<T, D, I8>& t, const char* blob, const PoolGeom& p, long long row) const {
+    const int lane = threadIdx.x & 31, r = lane >> 2, c = lane & 3;
+    if (row < 0) row = 0;
+    const char* base = blob + (row + r) * S::ROWB + c * 16;
+#pragma unroll
+    for (int i = 0; i < 2; ++i)
+#pragma unroll
+      for (int j = 0; j < S::CK; ++j) t.k[i][j] = ldg16(base + i * 8 * S::ROWB + j * 64);
+    if constexpr (I8) {
+#pragma unroll
+      for (int i = 0; i < 2; ++i) {
+        t.ks[i] = ldg_f32(reinterpret_cast<const float*>(blob + p.ks_off) + row + r + 8 * i);
+        t.vs[i] = ldg_f32(reinterpret_cast<const float*>(blob + p.vs_off) + row + r + 8 * i);
+      }
+    }
+  }
+  __device__ __forceinline__ void load_v(TileRegs<T, D, I8>& t, const char* blob, const PoolGeom& p, long long row) const {
+    const int lane = threadIdx.x & 31, r = lane >> 2, c = lane & 3;
+    if (row < 0) row = 0;
+    const char* base = blob + p.v_off + row * S::ROWB + r * S::VB;
+#pragma unroll
+    for (int i = 0; i < 4; ++i)
+#pragma unroll
+      for (int j = 0; j < S::CV; ++j) {
+        const char* at = base + v_row(c, i) * S::ROWB + j * 8 * S::VB;
+        if constexpr (S::VB == 16) t.v[i][j] = ldg16(at);
+        else { const uint2 w = ldg8(at); t.v[i][j] = make_uint4(w.x, w.y, 0, 0); }
+      }
+  }
+
+  __device__ __forceinline__ void scores(const TileRegs<T, D, I8>& t, float (&s)[NT][4]) const {
+#pragma unroll
+    for (int n = 0; n < NT; ++n)
+#pragma unroll
+      for (int i = 0; i < 4; ++i) s[n][i] = 0.f;
+#pragma unroll
+    for (int j = 0; j < S::CK; ++j) {
+      const uint32_t k0[4] = {t.k[0][j].x, t.k[0][j].y, t.k[0][j].z, t.k[0][j].w}, k1[4] = {t.k[1][j].x, t.k[1][j].y, t.k[1][j].z, t.k[1][j].w};
+      if constexpr (!I8) {
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+          const uint32_t a[4] = {k0[2 * h], k1[2 * h], k0[2 * h + 1], k1[2 * h + 1]};
+#pragma unroll
+          for (int n = 0; n < NT; ++n) {
+            if constexpr (S::F32) mma_3tf32(s[n], a, qf[n][4 * j + 2 * h], qf[n][4 * j + 2 * h + 1]);
+            else mma_bf16(s[n], a, qf[n][4 * j + 2 * h], qf[n][4 * j + 2 * h + 1]);
+          }
+        }
+      } else {
+#pragma unroll
+        for (int w = 0; w < 4; ++w) {
+          const uint32_t x0 = k0[w] ^ 0x80808080u, x1 = k1[w] ^ 0x80808080u;
+          const uint32_t a[4] = {codes_f16<0x4140>(x0), codes_f16<0x4140>(x1), codes_f16<0x4342>(x0), codes_f16<0x4342>(x1)};
+#pragma unroll
+          for (int n = 0; n < NT; ++n)
+#pragma unroll
+            for (int q = 0; q < S::QP; ++q) mma_f16(s[n], a, qf[n][q * 2 * S::KS + 2 * (4 * j + w)], qf[n][q * 2 * S::KS + 2 * (4 * j + w) + 1]);
+        }
+      }
+    }
+  }
+
+  // Scores -> probabilities (kept as the weights of the values' product in s), references and sums.  lim: rows of the tile that count.
+  __device__ __forceinline__ void weigh(const TileRegs<T, D, I8>& t, float (&s)[NT][4], int lim) {
+    const int r = (threadIdx.x & 31) >> 2;
+    const bool in0 = r < lim, in1 = r + 8 < lim;
+    constexpr float kGrow = 8.f, kRoom = 7.f;
+    float lv[2];
+    if constexpr (I8) { lv[0] = log2f(t.vs[0]); lv[1] = log2f(t.vs[1]); }
+    bool grow = false;
+    float y[NT][4];                                          // 8 bits: log2 of the weight p * (value's scale), in units of 2^m
+#pragma unroll
+    for (int n = 0; n < NT; ++n) {
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        const bool in = i < 2 ? in0 : in1;
+        float x = s[n][i] * hf[n][i & 1];
+        if constexpr (I8) x = s[n][i] * (hf[n][i & 1] * t.ks[i >> 1]);
+        s[n][i] = in ? x : -INFINITY;
+        // (the difference first: a scale's logarithm would be lost in a large score)
+        if constexpr (I8) y[n][i] = in ? (x - m[n][i & 1]) + lv[i >> 1] : -INFINITY;
+      }
+#pragma unroll
+      for (int i = 0; i < 2; ++i) {
+        grow |= fmaxf(s[n][i], s[n][i + 2]) > m[n][i] + kGrow;
+        if constexpr (I8) grow |= fmaxf(y[n][i], y[n][i + 2]) > m2[n][i] + kGrow;
+      }
+    }
+    // A reference moves only when a score is more than 2^8 above it (or it is the first), for all heads at once.
+    if (__any_sync(0xffffffffu, grow)) {
+#pragma unroll
+      for (int n = 0; n < NT; ++n)
+#pragma unroll
+        for (int i = 0; i < 2; ++i) {
+          float a = fmaxf(s[n][i], s[n][i + 2]);
+#pragma unroll
+          for (int o = 4; o < 32; o <<= 1) a = fmaxf(a, __shfl_xor_sync(0xffffffffu, a, o));
+          const float mn = fmaxf(m[n][i], a), shift = mn == m[n][i] ? 0.f : m[n][i] - mn, f = fast_exp2(shift);
+          m[n][i] = mn;
+          l[n][i] *= f;
+          float fo = f;
+          if constexpr (I8) {
+#pragma unroll
+            for (int k = 0; k < 2; ++k) y[n][i + 2 * k] = (k ? in1 : in0) ? (s[n][i + 2 * k] - mn) + lv[k] : -INFINITY;
+            float b = fmaxf(y[n][i], y[n][i + 2]);
+#pragma unroll
+            for (int o = 4; o < 32; o <<= 1) b = fmaxf(b, __shfl_xor_sync(0xffffffffu, b, o));
+            const float was = m2[n][i] + shift, mn2 = fmaxf(was, b);
+            fo = mn2 == -INFINITY ? 1.f : fast_exp2(was - mn2);
+            m2[n][i] = mn2;
+          }
+#pragma unroll
+          for (int u = 0; u < S::MT; ++u) { acc[n][u][i] *= fo; acc[n][u][i + 2] *= fo; }
+        }
+    }
+#pragma unroll
+    for (int n = 0; n < NT; ++n)
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        const bool in = i < 2 ? in0 : in1;
+        const float e = in ? fast_exp2(s[n][i] - m[n][i & 1]) : 0.f;
+        l[n][i & 1] += e;
+        s[n][i] = e;
+        // (a reference of -inf: every value so far is zero, or not a number)
+        if constexpr (I8) s[n][i] = !in ? 0.f : m2[n][i & 1] > -INFINITY ? fast_exp2(y[n][i] - (m2[n][i & 1] - kRoom)) : t.vs[i >> 1];
+      }
+  }
+
+  __device__ __forceinline__ void product(const TileRegs<T, D, I8>& t, const float (&s)[NT][4], int lim) {
+    const int lane = threadIdx.x & 31, r = lane >> 2, c = lane & 3;
+    // weights: keys on the rows -> keys side by side
+    uint32_t b[NT][S::QP][4];
+#pragma unroll
+    for (int n = 0; n < NT; ++n) {
+      if constexpr (S::F32) {
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {                        // key c + 4 i of head r
+          const int src = ((c + 4 * i) & 7) * 4 + (r >> 1);
+          const float e0 = __shfl_sync(0xffffffffu, s[n][2 * (i >> 1)], src), e1 = __shfl_sync(0xffffffffu, s[n][2 * (i >> 1) + 1], src);
+          b[n][0][i] = __float_as_uint(r & 1 ? e1 : e0);
+        }
+      } else {
+#pragma unroll
+        for (int i = 0; i < 2; ++i) {
+          if constexpr (I8) {
+            const uint32_t w = pack_f16x2(s[n][2 * i], s[n][2 * i + 1]);
+            b[n][0][i] = transpose8(w);
+            if constexpr (S::QP == 2) b[n][1][i] = transpose8(pack_f16x2(s[n][2 * i] - f16_lo(w), s[n][2 * i + 1] - f16_hi(w)));
+          } else {
+            b[n][0][i] = transpose8(pack_bf16x2(s[n][2 * i], s[n][2 * i + 1]));
+          }
+        }
+      }
+    }
+    uint4 v[4][S::CV];
+#pragma unroll
+    for (int i = 0; i < 4; ++i)
+#pragma unroll
+      for (int j = 0; j < S::CV; ++j) v[i][j] = t.v[i][j];
+    if (!I8 && lim < 16) {                                   // what lies behind the end may be anything: a NaN times zero would stay
+#pragma unroll
+      for (int i = 0; i < 4; ++i)
+        if (v_row(c, i) >= lim) {
+#pragma unroll
+          for (int j = 0; j < S::CV; ++j) v[i][j] = make_uint4(0, 0, 0, 0);
+        }
+    }
+#pragma unroll
+    for (int j = 0; j < S::CV; ++j) {
+      const uint32_t w[4][4] = {{v[0][j].x, v[0][j].y, v[0][j].z, v[0][j].w}, {v[1][j].x, v[1][j].y, v[1][j].z, v[1][j].w},
+                                {v[2][j].x, v[2][j].y, v[2][j].z, v[2][j].w}, {v[3][j].x, v[3][j].y, v[3][j].z, v[3][j].w}};
+      if constexpr (S::F32) {
+#pragma unroll
+        for (int u = 0; u < 2; ++u)                          // channels 32 j + 4 r + 2 u, + 1
+#pragma unroll
+          for (int g = 0; g < 2; ++g) {                      // keys 8 g ..
+            const uint32_t a[4] = {w[2 * g][2 * u], w[2 * g][2 * u + 1], w[2 * g + 1][2 * u], w[2 * g + 1][2 * u + 1]};
+#pragma unroll
+            for (int n = 0; n < NT; ++n) mma_3tf32(acc[n][2 * j + u], a, b[n][0][2 * g], b[n][0][2 * g + 1]);
+          }
+      } else if constexpr (!I8) {
+#pragma unroll
+        for (int u = 0; u < 4; ++u) {                        // channels 64 j + 8 r + 2 u, + 1
+          const uint32_t a[4] = {__byte_perm(w[0][u], w[1][u], 0x5410), __byte_perm(w[0][u], w[1][u], 0x7632),
+                                 __byte_perm(w[2][u], w[3][u], 0x5410), __byte_perm(w[2][u], w[3][u], 0x7632)};
+#pragma unroll
+          for (int n = 0; n < NT; ++n) mma_bf16(acc[n][4 * j + u], a, b[n][0][0], b[n][0][1]);
+        }
+      } else {
+#pragma unroll
+        for (int u = 0; u < S::VB / 4; ++u) {                // channels E r + 4 u + 2 g, + 1
+          uint32_t x[4];
+#pragma unroll
+          for (int i = 0; i < 4; ++i) x[i] = w[i][u] ^ 0x80808080u;
+#pragma unroll
+          for (int g = 0; g < 2; ++g) {
+            const uint32_t p0 = g ? __byte_perm(x[0], x[1], 0x7362) : __byte_perm(x[0], x[1], 0x5140);
+            const uint32_t p1 = g ? __byte_perm(x[2], x[3], 0x7362) : __byte_perm(x[2], x[3], 0x5140);
+            const uint32_t a[4] = {codes_f16<0x4140>(p0), codes_f16<0x4342>(p0), codes_f16<0x4140>(p1), codes_f16<0x4342>(p1)};
+#pragma unroll
+            for (int n = 0; n < NT; ++n)
+#pragma unroll
+              for (int q = 0; q < S::QP; ++q) mma_f16(acc[n][2 * u + g], a, b[n][q][0], b[n][q][1]);
+          }
+        }
+      }
+    }
+  }
+
+  // Sums over the lanes that share a head; the output in units of 2^m.
+  __device__ __forceinline__ void finish() {
+#pragma unroll
+    for (int n = 0; n < NT; ++n)
+#pragma unroll
+      for (int i = 0; i < 2; ++i) {
+#pragma unroll
+        for (int o = 4; o < 32; o <<= 1) l[n][i] += __shfl_xor_sync(0xffffffffu, l[n][i], o);
+        if constexpr (I8) {
+          const float f = m2[n][i] == -INFINITY ? 1.f : exp2f(m2[n][i] - 7.f);
+#pragma unroll
+          for (int u = 0; u < S::MT; ++u) { acc[n][u][i] *= f; acc[n][u][i + 2] *= f; }
+        }
+      }
+  }
+  // first channel of block u
+  static __device__ __forceinline__ int channel(int u) {
+    const int r = (threadIdx.x & 31) >> 2;
+    constexpr int per = S::E / 2;
+    return u / per * (8 * S::E) + S::E * r + 2 * (u % per);
+  }
+};
+
+// Pieces are joined as o = sum_i 2^(m_i - m) o_i, l likewise.  A piece: [heads][decode_row(D)], a row is O, then m and l.
+template <typename T, int D, bool I8, int NT>
+__global__ void __launch_bounds__(kDecodeThreads, 1) pool_decode_kernel(const T* __restrict__ q, long long q_stride,
+                                                                     const T* __restrict__ k_new, const T* __restrict__ v_new,
+                                                                     long long kv_stride, const int* __restrict__ table,
+                                                                     int table_stride, const int* __restrict__ lens, int n_seqs,
+                                                                     char* blob, char* __restrict__ ws, T* __restrict__ out,
+                                                                     float* __restrict__ lse, PoolGeom p) {
+  using S = DecodeShape<T, D, I8>;
+  constexpr int H = 8 * NT, RS = decode_row(D), LANES = D / Piece<T>::N;
+  extern __shared__ __align__(16) float smem_f[];
+  float* pieces = smem_f;                                    // [warps][2][H][RS]
+  int* pre = reinterpret_cast<int*>(smem_f + kDecodeWarps * 2 * H * RS);   // [n_seqs + 1] tiles of one head before a sequence
+  __shared__ int s_seg[kDecodeWarps][2], s_scan[kDecodeWarps + 1], s_last;
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  const int HG = (p.G + H - 1) / H, HH = p.Hkv * HG;
+  int* counters = reinterpret_cast<int*>(ws + kWsHeaderBytes);
+  float* joints = reinterpret_cast<float*>(ws + p.joints_off);
+
+  // ---- the line of work
+  const int room = static_cast<int>((static_cast<long long>(table_stride) << p.ps_log2) - (k_new ? 1 : 0));
+  auto length = [&](int seq, bool tell) {                    // rows of the sequence, its new one included
+    int len = lens[seq];
+    if (len < 0 || len > room) { if (tell) pool_refuse(ws); len = len < 0 ? 0 : room; }
+    return len + (k_new ? 1 : 0);
+  };
+  if (threadIdx.x < kDecodeWarps * 2) s_seg[threadIdx.x >> 1][threadIdx.x & 1] = -1;
+  int carry = 0;
+  for (int i0 = 0; i0 < n_seqs; i0 += kDecodeThreads) {
+    const int i = i0 + threadIdx.x;
+    int x = i < n_seqs ? (length(i, blockIdx.x == 0) + 15) >> 4 : 0;
+#pragma unroll
+    for (int o = 1; o < 32; o <<= 1) { const int y = __shfl_up_sync(0xffffffffu, x, o); if (lane >= o) x += y; }
+    if (lane == 31) s_scan[warp] = x;
+    __syncthreads();
+    int before = carry, all = 0;
+    for (int w = 0; w < kDecodeWarps; ++w) { if (w < warp) before += s_scan[w]; all += s_scan[w]; }
+    if (i < n_seqs) pre[i + 1] = before + x;
+    carry += all;
     __syncthreads();
   }
-  float qv[8][E], m[8], l[8], acc[8][E];
-#pragma unroll
-  for (int h = 0; h < 8; ++h) {
-    m[h] = -INFINITY; l[h] = 0.f;
-#pragma unroll
-    for (int i = 0; i < E; ++i) {
-      acc[h][i] = 0.f;
-      qv[h][i] = h < heads ? static_cast<float>(q[seq * q_stride + static_cast<long long>(g * p.G + h0 + h) * D + lane * E + i]) * p.scale_log2 : 0.f;
-    }
+  if (threadIdx.x == 0) pre[0] = 0;
+  __syncthreads();
+  const long long total = static_cast<long long>(carry) * HH;
+  long long per = (total + gridDim.x - 1) / gridDim.x;
+  if (per < p.min_tiles) per = p.min_tiles;
+  const long long a = min(per * blockIdx.x, total), e = min(a + per, total);
+
+  // sequences without a row
+  for (int i = blockIdx.x; i < n_seqs; i += gridDim.x)
+    if (pre[i + 1] == pre[i])
+      for (int x = threadIdx.x; x < p.Hq * D; x += kDecodeThreads) {
+        out[static_cast<long long>(i) * p.Hq * D + x] = static_cast<T>(0.f);
+        if (lse && x < p.Hq) lse[static_cast<long long>(i) * p.Hq + x] = -INFINITY;
+      }
+
+  // ---- this warp's pieces
+  long long x = a + (e - a) * warp / kDecodeWarps;
+  const long long x_end = a + (e - a) * (warp + 1) / kDecodeWarps;
+  int seq = 0;
+  if (x < x_end) {                                           // the sequence that holds tile x: the last whose tiles begin at or before it
+    int hi = n_seqs;
+    while (hi - seq > 1) { const int mid = (seq + hi) >> 1; if (static_cast<long long>(pre[mid]) * HH <= x) seq = mid; else hi = mid; }
   }
-  for (long long j = warp; j < len; j += kDecodeWarps) {
-    const long long row = row_of(j);
-    if (row < 0) { if (lane == 0) pool_refuse(ws); continue; }
-    float kx[E], vx[E];
-    key_values<T, D, I8>(blob, ks, row, lane, kx);
-    key_values<T, D, I8>(blob + p.v_off, vs, row, lane, vx);
-#pragma unroll
-    for (int h = 0; h < 8; ++h) {
-      float s = 0.f;
-#pragma unroll
-      for (int i = 0; i < E; ++i) s = fmaf(qv[h][i], kx[i], s);
-#pragma unroll
-      for (int o = 16; o > 0; o >>= 1) s += __shfl_xor_sync(0xffffffffu, s, o);
-      const float mn = fmaxf(m[h], s), f = m[h] == -INFINITY ? 0.f : exp2f(m[h] - mn), e = mn == -INFINITY ? 0.f : exp2f(s - mn);
-      m[h] = mn;
-      l[h] = fmaf(l[h], f, e);
-#pragma unroll
-      for (int i = 0; i < E; ++i) acc[h][i] = fmaf(acc[h][i], f, e * vx[i]);
+  bool first_piece = true;
+  while (x < x_end) {
+    const int tiles = pre[seq + 1] - pre[seq];
+    if (tiles == 0) { ++seq; continue; }
+    const long long rel = x - static_cast<long long>(pre[seq]) * HH;
+    if (rel >= static_cast<long long>(tiles) * HH) { ++seq; continue; }
+    const int hh = static_cast<int>(rel / tiles), t0 = static_cast<int>(rel - static_cast<long long>(hh) * tiles);
+    const int t1 = static_cast<int>(min(static_cast<long long>(tiles), t0 + (x_end - x)));
+    const int g = hh / HG, h0 = (hh - g * HG) * H, heads = min(H, p.G - h0);
+    const int n = length(seq, false);
+    const int* pages = table + static_cast<long long>(seq) * table_stride;
+    Decoder<T, D, I8, NT> dec;
+    TileRegs<T, D, I8> tr;
+    int window = t0, page = -1;                              // a lane holds the page of tile window + lane
+    auto fetch_pages = [&](int t) {
+      window = t;
+      page = -1;
+      if (t + lane < t1) {
+        page = pages[(t + lane) >> (p.ps_log2 - 4)];
+        if (page < 0 || page >= p.n_pages) { page = -1; pool_refuse(ws); }
+      }
+    };
+    auto row_of = [&](int t) -> long long {
+      if (t - window >= 32) fetch_pages(t);
+      const int pg = __shfl_sync(0xffffffffu, page, t - window);
+      return pg < 0 ? -1 : ((static_cast<long long>(pg) * p.Hkv + g) << p.ps_log2) + ((t << 4) & ((1 << p.ps_log2) - 1));
+    };
+    fetch_pages(t0);
+    dec.begin(q + seq * q_stride + static_cast<long long>(g * p.G + h0) * D, heads, p.scale_log2);
+    auto append = [&](int t, long long row) {                // the token's own row (every head group writes the same bytes)
+      if (k_new && t == tiles - 1) {
+        const int piece = lane % LANES;
+        const long long src = seq * kv_stride + static_cast<long long>(g) * D + piece * Piece<T>::N;
+        const long long to = lane < LANES && row >= 0 ? row + ((n - 1) & 15) : -1;
+        put_row<T, D, I8>(blob, reinterpret_cast<float*>(blob + p.ks_off), to, piece, *reinterpret_cast<const uint4*>(k_new + src));
+        put_row<T, D, I8>(blob + p.v_off, reinterpret_cast<float*>(blob + p.vs_off), to, piece, *reinterpret_cast<const uint4*>(v_new + src));
+        __syncwarp();
+      }
+    };
+    long long row = row_of(t0);
+    append(t0, row);
+    dec.load_k(tr, blob, p, row);
+    dec.load_v(tr, blob, p, row);
+    for (int t = t0; t < t1; ++t) {
+      const int lim = row < 0 ? 0 : min(16, n - 16 * t);
+      float s[NT][4];
+      dec.scores(tr, s);
+      dec.weigh(tr, s, lim);
+      const bool more = t + 1 < t1;
+      if (more) {
+        row = row_of(t + 1);
+        append(t + 1, row);
+        dec.load_k(tr, blob, p, row);
+      }
+      dec.product(tr, s, lim);
+      if (more) dec.load_v(tr, blob, p, row);
     }
-  }
+    dec.finish();
+    const int c = lane & 3;
+    if (t0 == 0 && t1 == tiles) {
 #pragma unroll
-  for (int h = 0; h < 8; ++h) {
-    if (lane == 0) { sM[warp][h] = m[h]; sL[warp][h] = l[h]; }
+      for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
-    for (int i = 0; i < E; ++i) sO[warp][h][lane * E + i] = acc[h][i];
+        for (int i = 0; i < 2; ++i) {
+          const int h = nt * 8 + 2 * c + i;
+          if (h >= heads) continue;
+          const long long to = static_cast<long long>(seq) * p.Hq + g * p.G + h0 + h;
+          const float sum = dec.l[nt][i], inv = sum != 0.f ? 1.f / sum : 0.f;     // (a NaN stays one)
+#pragma unroll
+          for (int u = 0; u < S::MT; ++u) {
+            T* dst = out + to * D + dec.channel(u);
+            const float o0 = dec.acc[nt][u][i] * inv, o1 = dec.acc[nt][u][i + 2] * inv;
+            if constexpr (sizeof(T) == 2) *reinterpret_cast<uint32_t*>(dst) = pack_bf16x2(o0, o1);
+            else *reinterpret_cast<float2*>(dst) = make_float2(o0, o1);
+          }
+          if (lse && lane < 4) lse[to] = sum != 0.f ? (dec.m[nt][i] + log2f(sum)) * 0.6931471805599453f : -INFINITY;
+        }
+    } else {
+      const int slot = first_piece ? 0 : 1;
+      first_piece = false;
+      float* dst = pieces + (warp * 2 + slot) * H * RS;
+#pragma unroll
+      for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+        for (int i = 0; i < 2; ++i) {
+          float* row_f = dst + (nt * 8 + 2 * c + i) * RS;
+#pragma unroll
+          for (int u = 0; u < S::MT; ++u) *reinterpret_cast<float2*>(row_f + dec.channel(u)) = make_float2(dec.acc[nt][u][i], dec.acc[nt][u][i + 2]);
+          if (lane < 4) *reinterpret_cast<float2*>(row_f + D) = make_float2(dec.m[nt][i], dec.l[nt][i]);
+        }
+      if (lane == 0) s_seg[warp][slot] = seq * HH + hh;
+    }
+    x += t1 - t0;
   }
   __syncthreads();
-  for (int i = threadIdx.x; i < heads * D; i += kDecodeWarps * 32) {
-    const int h = i / D, c = i % D;
-    float mx = -INFINITY, sum = 0.f, o = 0.f;
-    for (int w = 0; w < kDecodeWarps; ++w) mx = fmaxf(mx, sM[w][h]);
-    for (int w = 0; w < kDecodeWarps; ++w) {
-      const float f = sM[w][h] == -INFINITY ? 0.f : exp2f(sM[w][h] - mx);
-      sum = fmaf(f, sL[w][h], sum);
-      o = fmaf(f, sO[w][h][c], o);
+
+  // ---- joining the pieces of a segment
+  auto give = [&](int sq, int hh, int h, int d4, float4 o, float m, float l) {      // a finished row's four channels
+    const int g = hh / HG, h0 = (hh - g * HG) * H;
+    const long long to = static_cast<long long>(sq) * p.Hq + g * p.G + h0 + h;
+    const float inv = l != 0.f ? 1.f / l : 0.f;
+    store4<T>(out + to * D + d4 * 4, make_float4(o.x * inv, o.y * inv, o.z * inv, o.w * inv));
+    if (lse && d4 == 0) lse[to] = l != 0.f ? (m + log2f(l)) * 0.6931471805599453f : -INFINITY;
+  };
+  const int* seg_of = &s_seg[0][0];
+  for (int i = 0; i < 2 * kDecodeWarps;) {
+    const int seg = seg_of[i];
+    if (seg < 0) { ++i; continue; }
+    int j = i + 1;                                           // pieces [i, j), some of which may be unused
+    while (j < 2 * kDecodeWarps && (seg_of[j] < 0 || seg_of[j] == seg)) ++j;
+    const int sq = seg / HH, hh = seg - sq * HH, tiles = pre[sq + 1] - pre[sq];
+    const long long s0 = static_cast<long long>(pre[sq]) * HH + static_cast<long long>(hh) * tiles, s1 = s0 + tiles;
+    const bool complete = s0 >= a && s1 <= e;
+    const int heads = min(H, p.G - hh % HG * H);
+    float* joint = joints + (static_cast<long long>(blockIdx.x) * 2 + (s0 >= a)) * kDecodePieceFloats;
+    for (int y = threadIdx.x; y < heads * (D / 4); y += kDecodeThreads) {
+      const int h = y / (D / 4), d4 = y % (D / 4);
+      float m = -INFINITY, l = 0.f;
+      float4 o = make_float4(0.f, 0.f, 0.f, 0.f);
+      for (int k = i; k < j; ++k)
+        if (seg_of[k] == seg) m = fmaxf(m, pieces[(k * H + h) * RS + D]);
+      for (int k = i; k < j; ++k) {
+        if (seg_of[k] != seg) continue;
+        const float* src = pieces + (k * H + h) * RS;
+        const float f = src[D] == -INFINITY ? 0.f : fast_exp2(src[D] - m);
+        const float4 v = *reinterpret_cast<const float4*>(src + d4 * 4);
+        l = fmaf(f, src[D + 1], l);
+        o.x = fmaf(f, v.x, o.x); o.y = fmaf(f, v.y, o.y); o.z = fmaf(f, v.z, o.z); o.w = fmaf(f, v.w, o.w);
+      }
+      if (complete) {
+        give(sq, hh, h, d4, o, m, l);
+      } else {
+        *reinterpret_cast<float4*>(joint + h * RS + d4 * 4) = o;
+        if (d4 == 0) *reinterpret_cast<float2*>(joint + h * RS + D) = make_float2(m, l);
+      }
     }
-    const long long to = static_cast<long long>(seq) * p.Hq + g * p.G + h0 + h;
-    out[to * D + c] = static_cast<T>(sum != 0.f ? o / sum : 0.f);      // (a NaN stays one)
-    if (c == 0 && lse) lse[to] = sum != 0.f ? (mx + log2f(sum)) * 0.6931471805599453f : -INFINITY;
+    i = j;
+    if (complete) continue;
+    // A segment of several CTAs: the one that comes last joins them all, in their order.
+    const int c0 = static_cast<int>(s0 / per), c1 = static_cast<int>((s1 - 1) / per);
+    __threadfence();
+    __syncthreads();
+    if (threadIdx.x == 0) {
+      s_last = atomicAdd(counters + seg, 1) == c1 - c0;
+      if (s_last) counters[seg] = 0;                         // as it was found
+    }
+    __syncthreads();
+    if (!s_last) continue;
+    __threadfence();
+    for (int y = threadIdx.x; y < heads * (D / 4); y += kDecodeThreads) {
+      const int h = y / (D / 4), d4 = y % (D / 4);
+      float m = -INFINITY, l = 0.f;
+      float4 o = make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll 8
+      for (int k = c0; k <= c1; ++k) {
+        const float* src = joints + (static_cast<long long>(k) * 2 + (k == c0)) * kDecodePieceFloats + h * RS;
+        const float4 v = __ldcg(reinterpret_cast<const float4*>(src + d4 * 4));
+        const float2 ml = __ldcg(reinterpret_cast<const float2*>(src + D));
+        const float mn = fmaxf(m, ml.x), f0 = mn == -INFINITY ? 0.f : fast_exp2(m - mn), f1 = mn == -INFINITY ? 0.f : fast_exp2(ml.x - mn);
+        m = mn;
+        l = fmaf(f1, ml.y, l * f0);
+        o.x = fmaf(f1, v.x, o.x * f0); o.y = fmaf(f1, v.y, o.y * f0); o.z = fmaf(f1, v.z, o.z * f0); o.w = fmaf(f1, v.w, o.w * f0);
+      }
+      give(sq, hh, h, d4, o, m, l);
+    }
   }
 }
 

@@ -73,7 +73,7 @@ extern "C" int kvc_pool_create(const kvc_pool_config* cfg, kvc_pool** out) {
   int ps_log2 = 4;
   while (ps_log2 <= 8 && (1 << ps_log2) != cfg->page_size) ++ps_log2;
   if (ps_log2 > 8) return KVC_EINVAL;
-  if (cfg->n_pages < 1 || cfg->max_seqs < 1 || cfg->max_seqs > 65535) return KVC_EINVAL;
+  if (cfg->n_pages < 1 || cfg->max_seqs < 1 || cfg->max_seqs > kvc::kDecodeMaxSeqs) return KVC_EINVAL;
   if (!(cfg->softmax_scale >= 0.f) || isinf(cfg->softmax_scale)) return KVC_EINVAL;
   if (cfg->device < 0 || cfg->device >= kMaxDevices || cfg->flags) return KVC_EINVAL;
   const double bytes = 2.0 * cfg->n_pages * cfg->n_kv_heads * cfg->page_size * cfg->head_dim * 4;
@@ -93,8 +93,13 @@ extern "C" int kvc_pool_create(const kvc_pool_config* cfg, kvc_pool** out) {
   g.scale_log2 = c->scale * 1.4426950408889634f;
   g.v_off = (long long)part; g.ks_off = (long long)(2 * part); g.vs_off = (long long)(2 * part + scales);
   c->blob_bytes = 2 * part + 2 * scales;
-  c->ws_clear = kvc::kWsHeaderBytes;
-  c->ws_bytes = c->ws_clear;
+  // workspace: status word, a counter per segment of kvc_pool_decode (a (sequence, kv-head, head group); groups of eight heads at
+  // least), and the pieces of segments that span CTAs, two per CTA
+  const size_t segments = (size_t)cfg->max_seqs * g.Hkv * ((g.G + 7) / 8);
+  c->ws_clear = align_up(kvc::kWsHeaderBytes + segments * 4, 256);
+  g.joints_off = (long long)c->ws_clear;
+  c->ws_bytes = c->ws_clear + (size_t)kvc::kDecodeMaxCtas * 2 * kvc::kDecodePieceFloats * 4;
+  g.min_tiles = 2 * kvc::kDecodeWarps;
   c->launches = 0;
   c->encode = nullptr;
   c->err[0] = 0;
@@ -148,6 +153,14 @@ static int check_rows(kvc_pool* c, const void* k, const void* v, long long ts, l
   if (!stride_ok(c, ts, cf.head_dim) || !stride_ok(c, hs, cf.head_dim))
     return fail(c, KVC_EINVAL, "strides %lld, %lld: multiples of 16 bytes, at least head_dim", ts, hs);
   return check_device(c);
+}
+
+template <typename Kernel>
+static cudaError_t opt_in_smem(Kernel kernel, int bytes, bool* done_per_device, int dev) {
+  if (done_per_device[dev]) return cudaSuccess;
+  const cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, bytes);
+  if (e == cudaSuccess) done_per_device[dev] = true;
+  return e;
 }
 
 template <typename F>
@@ -212,12 +225,27 @@ extern "C" int kvc_pool_decode(kvc_pool* c, const void* q, long long q_stride, c
   if (k_new && !stride_ok(c, kv_stride, (long long)cf.n_kv_heads * cf.head_dim)) return fail(c, KVC_EINVAL, "kv_stride = %lld", kv_stride);
   if (int rc = check_device(c)) return rc;
   if (n_seqs == 0) return KVC_OK;
+  // every (sequence, kv-head, head group) may be as long as the table
+  const long long most = (long long)n_seqs * cf.n_kv_heads * ((c->geom.G + 7) / 8) * ((((long long)table_stride << c->geom.ps_log2) + 15) / 16);
+  if (most > 0x7fffffffll) return fail(c, KVC_EINVAL, "%d sequences of up to %d pages: 2^31 tiles of work or more", n_seqs, table_stride);
   const cudaError_t e = by_shape(c, [&](auto t, auto d, auto i8) {
     using T = decltype(t);
     constexpr int D = decltype(d)::value;
-    kvc::pool_decode_kernel<T, D, decltype(i8)::value><<<dim3(n_seqs, cf.n_kv_heads, (c->geom.G + 7) / 8), kvc::kDecodeWarps * 32, 0, (cudaStream_t)stream>>>(
-        (const T*)q, q_stride, (const T*)k_new, (const T*)v_new, kv_stride, table, table_stride, lens, (char*)blob, (char*)workspace, (T*)out, lse, c->geom);
-    return cudaGetLastError();
+    constexpr bool I8 = decltype(i8)::value;
+    auto go = [&](auto nt) {
+      constexpr int NT = decltype(nt)::value;
+      auto kernel = kvc::pool_decode_kernel<T, D, I8, NT>;
+      const int base = kvc::kDecodeWarps * 2 * 8 * NT * kvc::decode_row(D) * 4, smem = base + (n_seqs + 1) * 4;
+      static bool attr_set[kMaxDevices] = {};
+      if (cudaError_t x = opt_in_smem(kernel, base + (kvc::kDecodeMaxSeqs + 1) * 4, attr_set, cf.device)) return x;
+      const int ctas = (int)std::max<long long>(1, std::min<long long>(kvc::kNumSMs, (most + c->geom.min_tiles - 1) / c->geom.min_tiles));
+      kernel<<<ctas, kvc::kDecodeThreads, smem, (cudaStream_t)stream>>>((const T*)q, q_stride, (const T*)k_new, (const T*)v_new, kv_stride, table,
+                                                                        table_stride, lens, n_seqs, (char*)blob, (char*)workspace, (T*)out, lse, c->geom);
+      return cudaGetLastError();
+    };
+    if constexpr (kvc::DecodeShape<T, D, I8>::NT == 2)
+      if (c->geom.G > 8) return go(std::integral_constant<int, 2>());
+    return go(std::integral_constant<int, 1>());
   });
   c->launches++;
   return check_cuda(c, e, "decode launch");
@@ -286,14 +314,6 @@ static int make_map(kvc_pool* c, CUtensorMap* m, const void* base, int d, int he
                                CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_128B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
   if (r != CUDA_SUCCESS) return fail(c, KVC_ECUDA, "cuTensorMapEncodeTiled failed (%d): %d heads, %lld tokens, stride %lld", (int)r, heads, tokens, stride);
   return KVC_OK;
-}
-
-template <typename Kernel>
-static cudaError_t opt_in_smem(Kernel kernel, int bytes, bool* done_per_device, int dev) {
-  if (done_per_device[dev]) return cudaSuccess;
-  const cudaError_t e = cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, bytes);
-  if (e == cudaSuccess) done_per_device[dev] = true;
-  return e;
 }
 
 template <int D, int R>
