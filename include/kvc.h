@@ -324,7 +324,7 @@ typedef struct {
   int page_format;     /* kvc_page_format                                                    */
   int page_size;       /* P: 16, 32, 64, 128 or 256 tokens                                   */
   int n_pages;         /* N >= 1                                                             */
-  int max_seqs;        /* most sequences of one kvc_pool_decode call, 1 .. 4096              */
+  int max_seqs;        /* most sequences of one kvc_pool_decode call, 1 .. 1024              */
   float softmax_scale; /* 0 -> 1/sqrt(head_dim)                                              */
   int device;          /* CUDA device ordinal                                                */
   unsigned flags;      /* 0                                                                  */

@@ -73,7 +73,8 @@ template <> struct Piece<__nv_bfloat16> {
 // The lanes that hold a row, one piece each, leave it in row `dst` of K or V pages.  All lanes of the warp call it (the ones of
 // a row agree on `dst`; negative: nothing is stored).
 template <typename T, int D, bool I8>
-__device__ __forceinline__ void put_row(char* codes, float* scales, long long dst, int piece, uint4 raw) {
+__device__ __forceinline__ void put_row(char* codes, float* scales, long long dst, int piece, uint4 raw, uint8_t* own_codes = nullptr,
+                                        float* own_scale = nullptr) {
   constexpr int N = Piece<T>::N, LANES = D / N;
   if constexpr (!I8) {
     if (dst >= 0) reinterpret_cast<uint4*>(codes)[dst * LANES + piece] = raw;
@@ -90,6 +91,11 @@ __device__ __forceinline__ void put_row(char* codes, float* scales, long long ds
 #pragma unroll
     for (int i = 0; i < N / 4; ++i)
       c[i] = row_code(x[4 * i], rs.inv) | row_code(x[4 * i + 1], rs.inv) << 8 | row_code(x[4 * i + 2], rs.inv) << 16 | row_code(x[4 * i + 3], rs.inv) << 24;
+    if (own_codes) {                                         // (kvc_pool_decode: the row is wanted at once)
+      if constexpr (N == 8) *reinterpret_cast<uint2*>(own_codes + piece * 8) = make_uint2(c[0], c[1]);
+      else *reinterpret_cast<uint32_t*>(own_codes + piece * 4) = c[0];
+      if (piece == 0) *own_scale = rs.s;
+    }
     if (dst >= 0) {
       if constexpr (N == 8) *reinterpret_cast<uint2*>(codes + dst * D + piece * 8) = make_uint2(c[0], c[1]);
       else *reinterpret_cast<uint32_t*>(codes + dst * D + piece * 4) = c[0];
@@ -194,16 +200,17 @@ __global__ void __launch_bounds__(kPoolThreads) pool_read_kernel(const char* __r
 // Mathematics: for every (sequence, kv-head) and its G query heads, s = scale * K q, o = V^T p / sum p with p = 2^(s - m) and a
 // running reference m.  Keys stand on the rows of the matrix instruction and query heads on its eight columns: S^T = K Q^T and
 // O^T = V^T P^T, so that up to eight heads cost one instruction where heads as rows would leave half of sixteen empty.
-// Bound: HBM, G FLOP per byte at bf16.  So pages go from global memory straight into the registers of the lane that feeds
-// them to the matrix instruction, 16 bytes per load: the order of a contraction is free, hence lane (r, c) = (lane / 4,
-// lane % 4) takes whole 16-byte pieces of a key's row, and the query's fragment is laid out the same way.  Values need
-// pairs of keys side by side (two bytes permutes per pair of words); eight lanes read a row's 128 bytes at once.
-// Neither shared memory nor a barrier is on the way, a tile's loads are issued while the one before is computed.
+// Bound: HBM, G FLOP per byte at bf16.  A warp has a ring of tiles in shared memory of its own (cp.async, whole stretches of a page;
+// rows behind a sequence's end become zeros without being read), so no warp waits for another.  The order of a contraction is free: a
+// lane (r, c) = (lane / 4, lane % 4) takes whole 16-byte pieces of the rows that its fragments need, and the query's fragment is
+// laid out the same way.  Values need pairs of keys side by side (two byte permutes per pair of words).
 //
 // Work: tiles of 16 keys of all (sequence, kv-head, head group) segments form one line, cut into equal ranges for the CTAs and
-// those for the warps, whatever the sequences' lengths (which only the device knows).  A warp that has a whole segment
-// writes its output; pieces are joined in shared memory, and pieces of a segment that spans CTAs in the workspace by the CTA that comes
-// last -- in the order of the pieces, so that results do not depend on who that is.
+// those for the warps, whatever the sequences' lengths (which only the device knows).  A warp's loads run ahead of its arithmetic across
+// the ends of segments.  A warp that has a whole segment writes its output; pieces are joined in shared memory, and pieces of a
+// segment that spans CTAs in the workspace by the CTA that comes last -- in the order of the pieces, so that results do not depend on
+// who that is.
+// The token's own row (k_new) is written to its page and loaded from where it came from, not back from the page.
 //
 // 8 bits: codes become fp16 exactly (1024 + 128 + c, less 1152, as bit patterns); a key's scale multiplies its score, a value's scale goes
 // into its weight p * s, with a reference 2^m2 of its own in units of 2^m (the largest weight is near 2^7, so that fp16 has room below).
@@ -212,6 +219,8 @@ __global__ void __launch_bounds__(kPoolThreads) pool_read_kernel(const char* __r
 // size of the output's own rounding), fp16 2^-12, and fp32 in two parts.
 // fp32 pages: three products of TF32 parts (x = hi + lo: hi hi + hi lo + lo hi, 2^-21 and below), sums in fp32.
 
+static constexpr int kDecodeMaxSeqs = 1024;                 // the sequences' tile counts are kept in shared memory
+static constexpr int kDecodeSmem = 232448 - 512 - (kDecodeMaxSeqs + 1) * 4 - kDecodeMaxSeqs;   // for the warps' rings and pieces
 template <typename T, int D, bool I8>
 struct DecodeShape {
   static constexpr bool F32 = sizeof(T) == 4 && !I8;        // fp32 pages
@@ -224,28 +233,24 @@ struct DecodeShape {
   static constexpr int MT = D / 16;                         // sixteen-channel blocks of the output
   static constexpr int QP = I8 && sizeof(T) == 4 ? 2 : 1;   // parts of a query or probability
   static constexpr int KS = F32 ? D / 8 : D / 16;           // steps of the contraction over channels
+  // tiles on their way per warp: what registers have room for
+  static constexpr int KB = 16 * ROWB;                      // bytes of a tile's keys, and of its values
+  static constexpr int STAGE = 2 * KB + (I8 ? 128 : 0);     // ... with the scales of both
+  static constexpr int OWN = I8 ? 2 * D + 16 : 0;           // the token's own row in codes, on its way to the lanes
+  template <int N> static __host__ __device__ constexpr int piece() { return 8 * N * (D + 4) * 4; }
+  template <int N> static __host__ __device__ constexpr int warps() { return F32 && D == 128 ? 5 : N == 2 || I8 ? 8 : 6; }
+  template <int N> static __host__ __device__ constexpr int stages() {
+    const int n = (kDecodeSmem / warps<N>() / 128 * 128 - piece<N>() - OWN) / STAGE;
+    return n < 8 ? n : 8;
+  }
+  // tiles that are computed together: two where the ring then still holds the next two
+  template <int N> static __host__ __device__ constexpr int unit() { return N == 1 && stages<N>() >= 4 ? 2 : 1; }
+  template <int N> static __host__ __device__ constexpr int warp_bytes() { return (stages<N>() * STAGE + OWN + piece<N>() + 127) / 128 * 128; }
 };
-static constexpr int kDecodeWarps = 8, kDecodeThreads = kDecodeWarps * 32;
 static constexpr int kDecodeMaxCtas = kNumSMs * 2;
-static constexpr int kDecodeMaxSeqs = 4096;                 // the sequences' tile counts are kept in shared memory
 __host__ __device__ constexpr int decode_row(int D) { return D + 4; }    // floats of a head's row of a piece: O, m, l
 static constexpr int kDecodePieceFloats = 16 * (128 + 4);   // a piece in the workspace: up to 16 heads
 
-__device__ __forceinline__ uint4 ldg16(const void* p) {      // read once: not kept in L1
-  uint4 r;
-  asm volatile("ld.global.L1::no_allocate.v4.u32 {%0, %1, %2, %3}, [%4];" : "=r"(r.x), "=r"(r.y), "=r"(r.z), "=r"(r.w) : "l"(p) : "memory");
-  return r;
-}
-__device__ __forceinline__ uint2 ldg8(const void* p) {
-  uint2 r;
-  asm volatile("ld.global.L1::no_allocate.v2.u32 {%0, %1}, [%2];" : "=r"(r.x), "=r"(r.y) : "l"(p) : "memory");
-  return r;
-}
-__device__ __forceinline__ float ldg_f32(const float* p) {
-  float r;
-  asm volatile("ld.global.f32 %0, [%1];" : "=f"(r) : "l"(p) : "memory");
-  return r;
-}
 __device__ __forceinline__ void mma_bf16(float* d, const uint32_t* a, uint32_t b0, uint32_t b1) {
   asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, {%0, %1, %2, %3};"
                : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3]) : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
@@ -293,13 +298,17 @@ template <uint32_t SEL> __device__ __forceinline__ uint32_t codes_f16(uint32_t x
   return r;
 }
 
-// What a lane holds of the sixteen keys and values of a tile.
-template <typename T, int D, bool I8> struct TileRegs {
-  using S = DecodeShape<T, D, I8>;
-  uint4 k[2][S::CK];               // rows r and r + 8
-  uint4 v[4][S::CV];               // rows 2c, 2c + 1, 2c + 8, 2c + 9 (fp32: c, c + 4, c + 8, c + 12)
-  float ks[2], vs[2];              // scales of rows r and r + 8
-};
+// cp.async of `bytes` of 16 (of 8, of 4); the rest is zeros
+__device__ __forceinline__ void copy16(uint32_t dst, const void* src, int bytes) {
+  asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(dst), "l"(src), "r"(bytes) : "memory");
+}
+__device__ __forceinline__ void copy8(uint32_t dst, const void* src, int bytes) {
+  asm volatile("cp.async.ca.shared.global [%0], [%1], 8, %2;" ::"r"(dst), "l"(src), "r"(bytes) : "memory");
+}
+__device__ __forceinline__ void copy4(uint32_t dst, const void* src, int bytes) {
+  asm volatile("cp.async.ca.shared.global [%0], [%1], 4, %2;" ::"r"(dst), "l"(src), "r"(bytes) : "memory");
+}
+__device__ __forceinline__ void prefetch_l1(const void* p) { asm volatile("prefetch.global.L1 [%0];" ::"l"(p)); }
 
 template <typename T, int D, bool I8, int NT>
 struct Decoder {
@@ -366,53 +375,79 @@ struct Decoder {
     }
   }
 
-  // row: first of the tile's sixteen rows in the pages (negative: none, the tile counts for nothing)
-  __device__ __forceinline__ void load_k(TileRegs<T, D, I8>& t, const char* blob, const PoolGeom& p, long long row) const {
-    const int lane = threadIdx.x & 31, r = lane >> 2, c = lane & 3;
-    if (row < 0) row = 0;
-    const char* base = blob + (row + r) * S::ROWB + c * 16;
-#pragma unroll
-    for (int i = 0; i < 2; ++i)
-#pragma unroll
-      for (int j = 0; j < S::CK; ++j) t.k[i][j] = ldg16(base + i * 8 * S::ROWB + j * 64);
-    if constexpr (I8) {
-#pragma unroll
-      for (int i = 0; i < 2; ++i) {
-        t.ks[i] = ldg_f32(reinterpret_cast<const float*>(blob + p.ks_off) + row + r + 8 * i);
-        t.vs[i] = ldg_f32(reinterpret_cast<const float*>(blob + p.vs_off) + row + r + 8 * i);
-      }
-    }
+  // A tile's stage in shared memory: row by row, sectors of 32 bytes exchanged so that the eight lanes of a read, and of a copy, meet
+  // all banks.  A sector stays whole, at a multiple of 32: copied to two places it is fetched twice (a ring that began at a
+  // multiple of 16, or pieces in the lanes' own order: twice the traffic from L2, 131k tokens, 32 / 8 heads 115 us).
+  static __device__ __forceinline__ int key_at(int row, int byte) {       // two rows of a read: two halves of 128 bytes
+    return row * S::ROWB + (S::ROWB >= 128 ? byte ^ ((row & 1) << 6) : byte);
   }
-  __device__ __forceinline__ void load_v(TileRegs<T, D, I8>& t, const char* blob, const PoolGeom& p, long long row) const {
-    const int lane = threadIdx.x & 31, r = lane >> 2, c = lane & 3;
-    if (row < 0) row = 0;
-    const char* base = blob + p.v_off + row * S::ROWB + r * S::VB;
-#pragma unroll
-    for (int i = 0; i < 4; ++i)
-#pragma unroll
-      for (int j = 0; j < S::CV; ++j) {
-        const char* at = base + v_row(c, i) * S::ROWB + j * 8 * S::VB;
-        if constexpr (S::VB == 16) t.v[i][j] = ldg16(at);
-        else { const uint2 w = ldg8(at); t.v[i][j] = make_uint4(w.x, w.y, 0, 0); }
-      }
+  static __device__ __forceinline__ int value_at(int row, int byte) {     // four rows of a read: four quarters
+    if (S::F32) return row * S::ROWB + (byte ^ ((row & 3) << 5));
+    return (row * S::ROWB + byte) ^ (((row >> 1) & 3) << 5);
   }
 
-  __device__ __forceinline__ void scores(const TileRegs<T, D, I8>& t, float (&s)[NT][4]) const {
+  // The sixteen rows of a tile are one stretch of its page: lane l copies pieces l, l + 32, ...
+  // kb, vb, sb: this lane's first piece of the tile in the pages.  lim: how many of the tile's rows count (the others become zeros);
+  // own: which of them is the token's own (16: none), at k_own, v_own in plain pages, in `codes` (K, V, their scales) in 8 bits.
+  template <bool WHOLE>
+  static __device__ __forceinline__ void load(uint8_t* stage, const char* kb, const char* vb, const char* sb, int lim, int own,
+                                              const char* k_own, const char* v_own, const uint8_t* codes) {
+    const int lane = threadIdx.x & 31;
+    const uint32_t to = smem_u32(stage);
+    constexpr int PR = S::ROWB / 16, RPI = 32 / PR;          // pieces of a row, rows per copy of the warp
+#pragma unroll
+    for (int m = 0; m < S::KB / 512; ++m) {
+      const int row = m * RPI + lane / PR, k = lane % PR, at = key_at(row, k * 16);
+      if (WHOLE) copy16(to + at, kb + m * 512, 16);
+      else if (row != own) copy16(to + at, kb + m * 512, row < lim ? 16 : 0);
+      else if (!I8) copy16(to + at, k_own + k * 16, 16);
+      else *reinterpret_cast<uint4*>(stage + at) = *reinterpret_cast<const uint4*>(codes + k * 16);
+    }
+    constexpr int PV = S::ROWB / S::VB, RPV = 32 / PV;
+#pragma unroll
+    for (int m = 0; m < S::KB / (32 * S::VB); ++m) {
+      const int row = m * RPV + lane / PV, k = lane % PV;
+      const int at = S::KB + value_at(row, k * S::VB);
+      const char* src = vb + m * (32 * S::VB);
+      int bytes = S::VB;
+      if (!WHOLE) {
+        if (row == own && I8) {
+          if constexpr (S::VB == 16) *reinterpret_cast<uint4*>(stage + at) = *reinterpret_cast<const uint4*>(codes + D + k * 16);
+          else *reinterpret_cast<uint2*>(stage + at) = *reinterpret_cast<const uint2*>(codes + D + k * 8);
+          continue;
+        }
+        if (row == own) src = v_own + k * S::VB;
+        else if (row >= lim) bytes = 0;
+      }
+      if constexpr (S::VB == 16) copy16(to + at, src, bytes); else copy8(to + at, src, bytes);
+    }
+    if constexpr (I8) {                                      // lanes 0 .. 15: keys' scales, 16 .. 31: values'
+      const int at = lane & 15;
+      if (!WHOLE && at == own) reinterpret_cast<float*>(stage + 2 * S::KB)[lane] = reinterpret_cast<const float*>(codes + 2 * D)[lane >> 4];
+      else copy4(to + 2 * S::KB + lane * 4, sb, WHOLE || at < lim ? 4 : 0);
+    }
+  }
+
+  // S^T of a tile.  A chain of dependent matrix instructions is what a warp waits for most: steps alternate between two sums.
+  __device__ __forceinline__ void scores(const uint8_t* stage, float (&s)[NT][4]) const {
+    const int r = (threadIdx.x & 31) >> 2, c = threadIdx.x & 3;
+    float part[2][NT][4];
 #pragma unroll
     for (int n = 0; n < NT; ++n)
 #pragma unroll
-      for (int i = 0; i < 4; ++i) s[n][i] = 0.f;
+      for (int i = 0; i < 4; ++i) part[0][n][i] = part[1][n][i] = 0.f;
 #pragma unroll
     for (int j = 0; j < S::CK; ++j) {
-      const uint32_t k0[4] = {t.k[0][j].x, t.k[0][j].y, t.k[0][j].z, t.k[0][j].w}, k1[4] = {t.k[1][j].x, t.k[1][j].y, t.k[1][j].z, t.k[1][j].w};
+      const uint4 w0 = *reinterpret_cast<const uint4*>(stage + key_at(r, c * 16 + j * 64)), w1 = *reinterpret_cast<const uint4*>(stage + key_at(r + 8, c * 16 + j * 64));
+      const uint32_t k0[4] = {w0.x, w0.y, w0.z, w0.w}, k1[4] = {w1.x, w1.y, w1.z, w1.w};
       if constexpr (!I8) {
 #pragma unroll
         for (int h = 0; h < 2; ++h) {
           const uint32_t a[4] = {k0[2 * h], k1[2 * h], k0[2 * h + 1], k1[2 * h + 1]};
 #pragma unroll
           for (int n = 0; n < NT; ++n) {
-            if constexpr (S::F32) mma_3tf32(s[n], a, qf[n][4 * j + 2 * h], qf[n][4 * j + 2 * h + 1]);
-            else mma_bf16(s[n], a, qf[n][4 * j + 2 * h], qf[n][4 * j + 2 * h + 1]);
+            if constexpr (S::F32) mma_3tf32(part[h][n], a, qf[n][4 * j + 2 * h], qf[n][4 * j + 2 * h + 1]);
+            else mma_bf16(part[h][n], a, qf[n][4 * j + 2 * h], qf[n][4 * j + 2 * h + 1]);
           }
         }
       } else {
@@ -423,80 +458,106 @@ struct Decoder {
 #pragma unroll
           for (int n = 0; n < NT; ++n)
 #pragma unroll
-            for (int q = 0; q < S::QP; ++q) mma_f16(s[n], a, qf[n][q * 2 * S::KS + 2 * (4 * j + w)], qf[n][q * 2 * S::KS + 2 * (4 * j + w) + 1]);
+            for (int q = 0; q < S::QP; ++q) mma_f16(part[w & 1][n], a, qf[n][q * 2 * S::KS + 2 * (4 * j + w)], qf[n][q * 2 * S::KS + 2 * (4 * j + w) + 1]);
         }
       }
     }
+#pragma unroll
+    for (int n = 0; n < NT; ++n)
+#pragma unroll
+      for (int i = 0; i < 4; ++i) s[n][i] = part[0][n][i] + part[1][n][i];
   }
 
-  // Scores -> probabilities (kept as the weights of the values' product in s), references and sums.  lim: rows of the tile that count.
-  __device__ __forceinline__ void weigh(const TileRegs<T, D, I8>& t, float (&s)[NT][4], int lim) {
-    const int r = (threadIdx.x & 31) >> 2;
-    const bool in0 = r < lim, in1 = r + 8 < lim;
+  // U tiles: scores, weights, references, product.  lim: rows of a tile that count (of one of them at least one).
+  // d = score - m (log2 units); in 8 bits the weight's logarithm is d + log2(value's scale) - m2.  (The difference first: a scale's
+  // logarithm would be lost in a large score.)
+  template <int U>
+  __device__ __forceinline__ void tiles(const uint8_t* const (&stage)[U], const int (&lim)[U]) {
+    const int lane = threadIdx.x & 31, r = lane >> 2, c = lane & 3;
     constexpr float kGrow = 8.f, kRoom = 7.f;
-    float lv[2];
-    if constexpr (I8) { lv[0] = log2f(t.vs[0]); lv[1] = log2f(t.vs[1]); }
-    bool grow = false;
-    float y[NT][4];                                          // 8 bits: log2 of the weight p * (value's scale), in units of 2^m
+    float x[U][NT][4], y[U][NT][4], lv[U][2], top = -INFINITY, top2 = -INFINITY;
 #pragma unroll
-    for (int n = 0; n < NT; ++n) {
+    for (int t = 0; t < U; ++t) {
+      scores(stage[t], x[t]);
+      float ks[2] = {1.f, 1.f};                              // scales of rows r and r + 8
+      if constexpr (I8) {
+        const float* scales = reinterpret_cast<const float*>(stage[t] + 2 * S::KB);
 #pragma unroll
-      for (int i = 0; i < 4; ++i) {
-        const bool in = i < 2 ? in0 : in1;
-        float x = s[n][i] * hf[n][i & 1];
-        if constexpr (I8) x = s[n][i] * (hf[n][i & 1] * t.ks[i >> 1]);
-        s[n][i] = in ? x : -INFINITY;
-        // (the difference first: a scale's logarithm would be lost in a large score)
-        if constexpr (I8) y[n][i] = in ? (x - m[n][i & 1]) + lv[i >> 1] : -INFINITY;
+        for (int i = 0; i < 2; ++i) { ks[i] = scales[r + 8 * i]; lv[t][i] = __log2f(scales[16 + r + 8 * i]); }
       }
 #pragma unroll
-      for (int i = 0; i < 2; ++i) {
-        grow |= fmaxf(s[n][i], s[n][i + 2]) > m[n][i] + kGrow;
-        if constexpr (I8) grow |= fmaxf(y[n][i], y[n][i + 2]) > m2[n][i] + kGrow;
+      for (int n = 0; n < NT; ++n)
+#pragma unroll
+        for (int i = 0; i < 4; ++i) x[t][n][i] *= I8 ? hf[n][i & 1] * ks[i >> 1] : hf[n][i & 1];
+      if (__builtin_expect(lim[t] < 16, 0)) {                // behind the end: nothing, whatever the zeros there gave
+#pragma unroll
+        for (int n = 0; n < NT; ++n)
+#pragma unroll
+          for (int i = 0; i < 4; ++i)
+            if (r + 8 * (i >> 1) >= lim[t]) x[t][n][i] = -INFINITY;
       }
     }
+#pragma unroll
+    for (int t = 0; t < U; ++t)
+#pragma unroll
+      for (int n = 0; n < NT; ++n)
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          const float d = x[t][n][i] - m[n][i & 1];
+          top = fmaxf(top, d);
+          if constexpr (I8) { y[t][n][i] = d + (lv[t][i >> 1] - m2[n][i & 1]); top2 = fmaxf(top2, y[t][n][i]); }
+        }
     // A reference moves only when a score is more than 2^8 above it (or it is the first), for all heads at once.
-    if (__any_sync(0xffffffffu, grow)) {
+    if (__builtin_expect(__any_sync(0xffffffffu, top > kGrow || (I8 && top2 > kGrow)), 0)) {
 #pragma unroll
       for (int n = 0; n < NT; ++n)
 #pragma unroll
         for (int i = 0; i < 2; ++i) {
-          float a = fmaxf(s[n][i], s[n][i + 2]);
+          float a = -INFINITY, b = -INFINITY;
+#pragma unroll
+          for (int t = 0; t < U; ++t) a = fmaxf(a, fmaxf(x[t][n][i], x[t][n][i + 2]));
 #pragma unroll
           for (int o = 4; o < 32; o <<= 1) a = fmaxf(a, __shfl_xor_sync(0xffffffffu, a, o));
-          const float mn = fmaxf(m[n][i], a), shift = mn == m[n][i] ? 0.f : m[n][i] - mn, f = fast_exp2(shift);
+          // (scores of -inf alone: a reference below all others, not -inf, so that the differences are numbers)
+          const float mn = fmaxf(fmaxf(m[n][i], a), -1e30f), shift = m[n][i] - mn, f = fast_exp2(shift);
           m[n][i] = mn;
           l[n][i] *= f;
           float fo = f;
           if constexpr (I8) {
 #pragma unroll
-            for (int k = 0; k < 2; ++k) y[n][i + 2 * k] = (k ? in1 : in0) ? (s[n][i + 2 * k] - mn) + lv[k] : -INFINITY;
-            float b = fmaxf(y[n][i], y[n][i + 2]);
+            for (int t = 0; t < U; ++t) b = fmaxf(b, fmaxf((x[t][n][i] - mn) + lv[t][0], (x[t][n][i + 2] - mn) + lv[t][1]));
 #pragma unroll
             for (int o = 4; o < 32; o <<= 1) b = fmaxf(b, __shfl_xor_sync(0xffffffffu, b, o));
-            const float was = m2[n][i] + shift, mn2 = fmaxf(was, b);
-            fo = mn2 == -INFINITY ? 1.f : fast_exp2(was - mn2);
+            const float was = m2[n][i] + shift, mn2 = fmaxf(fmaxf(was, b), -1e30f);
+            fo = fast_exp2(was - mn2);
             m2[n][i] = mn2;
+#pragma unroll
+            for (int t = 0; t < U; ++t)
+#pragma unroll
+              for (int k = 0; k < 2; ++k) y[t][n][i + 2 * k] = (x[t][n][i + 2 * k] - mn) + lv[t][k] - mn2;
           }
 #pragma unroll
           for (int u = 0; u < S::MT; ++u) { acc[n][u][i] *= fo; acc[n][u][i + 2] *= fo; }
         }
     }
 #pragma unroll
-    for (int n = 0; n < NT; ++n)
+    for (int t = 0; t < U; ++t) {
 #pragma unroll
-      for (int i = 0; i < 4; ++i) {
-        const bool in = i < 2 ? in0 : in1;
-        const float e = in ? fast_exp2(s[n][i] - m[n][i & 1]) : 0.f;
-        l[n][i & 1] += e;
-        s[n][i] = e;
-        // (a reference of -inf: every value so far is zero, or not a number)
-        if constexpr (I8) s[n][i] = !in ? 0.f : m2[n][i & 1] > -INFINITY ? fast_exp2(y[n][i] - (m2[n][i & 1] - kRoom)) : t.vs[i >> 1];
-      }
+      for (int n = 0; n < NT; ++n)
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          const float e = fast_exp2(x[t][n][i] - m[n][i & 1]);
+          l[n][i & 1] += e;
+          x[t][n][i] = I8 ? fast_exp2(y[t][n][i] + kRoom) : e;
+        }
+      product(stage[t], x[t]);
+    }
+    (void)c;
   }
 
-  __device__ __forceinline__ void product(const TileRegs<T, D, I8>& t, const float (&s)[NT][4], int lim) {
+  __device__ __forceinline__ void product(const uint8_t* stage, const float (&s)[NT][4]) {
     const int lane = threadIdx.x & 31, r = lane >> 2, c = lane & 3;
+    (void)r; (void)c;
     // weights: keys on the rows -> keys side by side
     uint32_t b[NT][S::QP][4];
 #pragma unroll
@@ -521,23 +582,19 @@ struct Decoder {
         }
       }
     }
-    uint4 v[4][S::CV];
-#pragma unroll
-    for (int i = 0; i < 4; ++i)
-#pragma unroll
-      for (int j = 0; j < S::CV; ++j) v[i][j] = t.v[i][j];
-    if (!I8 && lim < 16) {                                   // what lies behind the end may be anything: a NaN times zero would stay
-#pragma unroll
-      for (int i = 0; i < 4; ++i)
-        if (v_row(c, i) >= lim) {
-#pragma unroll
-          for (int j = 0; j < S::CV; ++j) v[i][j] = make_uint4(0, 0, 0, 0);
-        }
-    }
 #pragma unroll
     for (int j = 0; j < S::CV; ++j) {
-      const uint32_t w[4][4] = {{v[0][j].x, v[0][j].y, v[0][j].z, v[0][j].w}, {v[1][j].x, v[1][j].y, v[1][j].z, v[1][j].w},
-                                {v[2][j].x, v[2][j].y, v[2][j].z, v[2][j].w}, {v[3][j].x, v[3][j].y, v[3][j].z, v[3][j].w}};
+      uint32_t w[4][4];
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        if constexpr (S::VB == 16) {
+          const uint4 x = *reinterpret_cast<const uint4*>(stage + S::KB + value_at(v_row(c, i), r * 16 + j * 128));
+          w[i][0] = x.x; w[i][1] = x.y; w[i][2] = x.z; w[i][3] = x.w;
+        } else {
+          const uint2 x = *reinterpret_cast<const uint2*>(stage + S::KB + value_at(v_row(c, i), r * 8));
+          w[i][0] = x.x; w[i][1] = x.y;
+        }
+      }
       if constexpr (S::F32) {
 #pragma unroll
         for (int u = 0; u < 2; ++u)                          // channels 32 j + 4 r + 2 u, + 1
@@ -585,7 +642,7 @@ struct Decoder {
 #pragma unroll
         for (int o = 4; o < 32; o <<= 1) l[n][i] += __shfl_xor_sync(0xffffffffu, l[n][i], o);
         if constexpr (I8) {
-          const float f = m2[n][i] == -INFINITY ? 1.f : exp2f(m2[n][i] - 7.f);
+          const float f = m2[n][i] == -INFINITY ? 1.f : exp2f(m2[n][i] - 7.f);   // (no tile)
 #pragma unroll
           for (int u = 0; u < S::MT; ++u) { acc[n][u][i] *= f; acc[n][u][i + 2] *= f; }
         }
@@ -601,51 +658,58 @@ struct Decoder {
 
 // Pieces are joined as o = sum_i 2^(m_i - m) o_i, l likewise.  A piece: [heads][decode_row(D)], a row is O, then m and l.
 template <typename T, int D, bool I8, int NT>
-__global__ void __launch_bounds__(kDecodeThreads, 1) pool_decode_kernel(const T* __restrict__ q, long long q_stride,
+__global__ void __launch_bounds__(DecodeShape<T, D, I8>::template warps<NT>() * 32, 1) pool_decode_kernel(const T* __restrict__ q, long long q_stride,
                                                                      const T* __restrict__ k_new, const T* __restrict__ v_new,
                                                                      long long kv_stride, const int* __restrict__ table,
                                                                      int table_stride, const int* __restrict__ lens, int n_seqs,
                                                                      char* blob, char* __restrict__ ws, T* __restrict__ out,
                                                                      float* __restrict__ lse, PoolGeom p) {
   using S = DecodeShape<T, D, I8>;
-  constexpr int H = 8 * NT, RS = decode_row(D), LANES = D / Piece<T>::N;
-  extern __shared__ __align__(16) float smem_f[];
-  float* pieces = smem_f;                                    // [warps][2][H][RS]
-  int* pre = reinterpret_cast<int*>(smem_f + kDecodeWarps * 2 * H * RS);   // [n_seqs + 1] tiles of one head before a sequence
-  __shared__ int s_seg[kDecodeWarps][2], s_scan[kDecodeWarps + 1], s_last;
+  using Dec = Decoder<T, D, I8, NT>;
+  constexpr int H = 8 * NT, RS = decode_row(D), LANES = D / Piece<T>::N, NS = S::template stages<NT>(), U = S::template unit<NT>(), AHEAD = NS - U,
+                WB = S::template warp_bytes<NT>();
+  constexpr int kDecodeWarps = S::template warps<NT>(), kDecodeThreads = kDecodeWarps * 32;
+  static_assert(NS >= 2 && NS * S::STAGE >= S::template piece<NT>(), "two tiles on their way; the last piece overlays the ring");
+  extern __shared__ __align__(128) uint8_t smem_b[];          // per warp: ring, own row, first piece; then the line of work
+  int* pre = reinterpret_cast<int*>(smem_b + kDecodeWarps * WB);           // [n_seqs + 1] tiles of one head before a sequence
+  uint8_t* last = reinterpret_cast<uint8_t*>(pre + n_seqs + 1);            // [n_seqs] rows of a sequence's last tile
+  __shared__ int s_seg[kDecodeWarps][2], s_scan[kDecodeWarps], s_last;
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  uint8_t* ring = smem_b + warp * WB;
+  uint8_t* own_codes = ring + NS * S::STAGE;
+  // piece 0 of warp w behind its ring, piece 1 over the ring
+  auto piece_at = [&](int i) { return reinterpret_cast<float*>(smem_b + (i >> 1) * WB + ((i & 1) ? 0 : NS * S::STAGE + S::OWN)); };
   const int HG = (p.G + H - 1) / H, HH = p.Hkv * HG;
   int* counters = reinterpret_cast<int*>(ws + kWsHeaderBytes);
   float* joints = reinterpret_cast<float*>(ws + p.joints_off);
 
-  // ---- the line of work
+  // ---- the line of work (the host has checked that it has fewer than 2^31 tiles)
   const int room = static_cast<int>((static_cast<long long>(table_stride) << p.ps_log2) - (k_new ? 1 : 0));
-  auto length = [&](int seq, bool tell) {                    // rows of the sequence, its new one included
-    int len = lens[seq];
-    if (len < 0 || len > room) { if (tell) pool_refuse(ws); len = len < 0 ? 0 : room; }
-    return len + (k_new ? 1 : 0);
-  };
   if (threadIdx.x < kDecodeWarps * 2) s_seg[threadIdx.x >> 1][threadIdx.x & 1] = -1;
-  int carry = 0;
+  if (threadIdx.x == 0) pre[0] = 0;
+  int sum = 0;
   for (int i0 = 0; i0 < n_seqs; i0 += kDecodeThreads) {
     const int i = i0 + threadIdx.x;
-    int x = i < n_seqs ? (length(i, blockIdx.x == 0) + 15) >> 4 : 0;
+    int x = 0;
+    if (i < n_seqs) {
+      int len = lens[i];
+      if (len < 0 || len > room) { if (blockIdx.x == 0) pool_refuse(ws); len = len < 0 ? 0 : room; }
+      if (k_new) ++len;                                      // rows of the sequence, its new one included
+      x = (len + 15) >> 4;
+      last[i] = static_cast<uint8_t>((len - 1) & 15) + 1;
+    }
 #pragma unroll
     for (int o = 1; o < 32; o <<= 1) { const int y = __shfl_up_sync(0xffffffffu, x, o); if (lane >= o) x += y; }
     if (lane == 31) s_scan[warp] = x;
     __syncthreads();
-    int before = carry, all = 0;
-    for (int w = 0; w < kDecodeWarps; ++w) { if (w < warp) before += s_scan[w]; all += s_scan[w]; }
+    int before = sum;
+    for (int w = 0; w < kDecodeWarps; ++w) { if (w < warp) before += s_scan[w]; sum += s_scan[w]; }
     if (i < n_seqs) pre[i + 1] = before + x;
-    carry += all;
     __syncthreads();
   }
-  if (threadIdx.x == 0) pre[0] = 0;
-  __syncthreads();
-  const long long total = static_cast<long long>(carry) * HH;
-  long long per = (total + gridDim.x - 1) / gridDim.x;
-  if (per < p.min_tiles) per = p.min_tiles;
-  const long long a = min(per * blockIdx.x, total), e = min(a + per, total);
+  const int total = sum * HH;
+  const int per = max((total + static_cast<int>(gridDim.x) - 1) / static_cast<int>(gridDim.x), p.min_tiles);
+  const int a = min(per * static_cast<int>(blockIdx.x), total), e = min(a + per, total);
 
   // sequences without a row
   for (int i = blockIdx.x; i < n_seqs; i += gridDim.x)
@@ -655,73 +719,132 @@ __global__ void __launch_bounds__(kDecodeThreads, 1) pool_decode_kernel(const T*
         if (lse && x < p.Hq) lse[static_cast<long long>(i) * p.Hq + x] = -INFINITY;
       }
 
-  // ---- this warp's pieces
-  long long x = a + (e - a) * warp / kDecodeWarps;
-  const long long x_end = a + (e - a) * (warp + 1) / kDecodeWarps;
-  int seq = 0;
-  if (x < x_end) {                                           // the sequence that holds tile x: the last whose tiles begin at or before it
+  // ---- this warp's tiles
+  const int x0 = a + (e - a) * warp / kDecodeWarps, x1 = a + (e - a) * (warp + 1) / kDecodeWarps;
+  struct Cursor { int left, seq, g, hg, t, tiles; };         // tile t of kv-head g, head group hg of a sequence; how many are left from it on
+  Cursor cur{x1 - x0, 0, 0, 0, 0, 0};
+  if (x0 < x1) {                                             // the sequence that holds tile x0: the last whose tiles begin at or before it
     int hi = n_seqs;
-    while (hi - seq > 1) { const int mid = (seq + hi) >> 1; if (static_cast<long long>(pre[mid]) * HH <= x) seq = mid; else hi = mid; }
+    while (hi - cur.seq > 1) { const int mid = (cur.seq + hi) >> 1; if (pre[mid] * HH <= x0) cur.seq = mid; else hi = mid; }
+    cur.tiles = pre[cur.seq + 1] - pre[cur.seq];
+    const int rel = x0 - pre[cur.seq] * HH;
+    const int hh = rel / cur.tiles;
+    cur.t = rel - hh * cur.tiles;
+    cur.g = hh / HG;
+    cur.hg = hh - cur.g * HG;
   }
+  auto step = [&](Cursor& x) {                               // on to the next tile
+    --x.left;
+    if (++x.t < x.tiles) return;
+    x.t = 0;
+    if (++x.hg < HG) return;
+    x.hg = 0;
+    if (++x.g < p.Hkv) return;
+    x.g = 0;
+    if (x.left > 0) { do { ++x.seq; x.tiles = pre[x.seq + 1] - pre[x.seq]; } while (x.tiles == 0); }
+  };
+  // loads run AHEAD tiles ahead
+  Cursor ld = cur;
+  uint32_t absent = 0;                                       // stages whose tile has no page
+  int ld_stage = 0, win_seq = -1, win = 0, page = -1;        // a lane holds the page of tile win + lane of sequence win_seq
+  const int c = lane & 3, page_rows = 1 << p.ps_log2;
+  const char* k_lane = blob + lane * 16;
+  const char* v_lane = blob + p.v_off + lane * S::VB;
+  const char* s_lane = blob + (lane < 16 ? p.ks_off : p.vs_off) + (lane & 15) * 4;
+  auto look = [&]() {                                        // pages of the tile to be loaded next, asked for a tile early
+    if (ld.left <= 0) return;
+    if (ld.seq != win_seq || static_cast<unsigned>(ld.t - win) >= 32u) {
+      win_seq = ld.seq; win = ld.t;
+      page = win + lane < ld.tiles ? table[static_cast<long long>(win_seq) * table_stride + ((win + lane) >> (p.ps_log2 - 4))] : 0;
+    }
+    if (ld.t == 0 || ld.left == x1 - x0) {                   // a segment's query
+      const int h0 = ld.hg * H, lines = (min(H, p.G - h0) * D * static_cast<int>(sizeof(T)) + 127) / 128;
+      const char* qs = reinterpret_cast<const char*>(q + ld.seq * q_stride + static_cast<long long>(ld.g * p.G + h0) * D);
+      if (lane < lines) prefetch_l1(qs + lane * 128);
+    }
+  };
+  auto load_next = [&]() {
+    if (ld.left > 0) {
+      const int pg = __shfl_sync(0xffffffffu, page, ld.t - win);
+      uint8_t* stage = ring + ld_stage * S::STAGE;
+      // (rows of a blob are fewer than 2^32)
+      const uint32_t row = ((static_cast<uint32_t>(pg) * p.Hkv + ld.g) << p.ps_log2) + ((ld.t << 4) & (page_rows - 1));
+      const bool end = ld.t == ld.tiles - 1, none = static_cast<unsigned>(pg) >= static_cast<unsigned>(p.n_pages);
+      if (__builtin_expect(!end && !none, 1)) {
+        Dec::template load<true>(stage, k_lane + static_cast<unsigned long long>(row) * S::ROWB, v_lane + static_cast<unsigned long long>(row) * S::ROWB,
+                                 s_lane + static_cast<unsigned long long>(row) * 4, 16, 16, nullptr, nullptr, nullptr);
+        absent &= ~(1u << ld_stage);
+      } else {
+        const unsigned long long at = none ? 0 : row;
+        const int lim = none ? 0 : end ? last[ld.seq] : 16;
+        int own = 16;
+        const char* k_own = nullptr;
+        const char* v_own = nullptr;
+        if (none && lane == 0) pool_refuse(ws);
+        absent = (absent & ~(1u << ld_stage)) | static_cast<uint32_t>(none) << ld_stage;
+        if (k_new && end && !none) {                         // (every head group writes the same bytes)
+          own = lim - 1;
+          const long long src = ld.seq * kv_stride + static_cast<long long>(ld.g) * D;
+          k_own = reinterpret_cast<const char*>(k_new + src);
+          v_own = reinterpret_cast<const char*>(v_new + src);
+          const int piece = lane % LANES;
+          const long long to = lane < LANES ? static_cast<long long>(row) + own : -1;
+          const uint4 kr = reinterpret_cast<const uint4*>(k_own)[piece], vr = reinterpret_cast<const uint4*>(v_own)[piece];
+          float* sc = reinterpret_cast<float*>(own_codes + 2 * D);
+          put_row<T, D, I8>(blob, reinterpret_cast<float*>(blob + p.ks_off), to, piece, kr, own_codes, sc);
+          put_row<T, D, I8>(blob + p.v_off, reinterpret_cast<float*>(blob + p.vs_off), to, piece, vr, own_codes + D, sc + 1);
+          __syncwarp();
+        }
+        Dec::template load<false>(stage, k_lane + at * S::ROWB, v_lane + at * S::ROWB, s_lane + at * 4, lim, own, k_own, v_own, own_codes);
+        if (I8 && own < 16) __syncwarp();                    // (the next own row may be written over this one)
+      }
+      if (++ld_stage == NS) ld_stage = 0;
+      step(ld);
+      look();
+    }
+    cp_async_commit();
+  };
+  look();
+#pragma unroll 1
+  for (int i = 0; i < AHEAD; ++i) load_next();
   bool first_piece = true;
-  while (x < x_end) {
-    const int tiles = pre[seq + 1] - pre[seq];
-    if (tiles == 0) { ++seq; continue; }
-    const long long rel = x - static_cast<long long>(pre[seq]) * HH;
-    if (rel >= static_cast<long long>(tiles) * HH) { ++seq; continue; }
-    const int hh = static_cast<int>(rel / tiles), t0 = static_cast<int>(rel - static_cast<long long>(hh) * tiles);
-    const int t1 = static_cast<int>(min(static_cast<long long>(tiles), t0 + (x_end - x)));
-    const int g = hh / HG, h0 = (hh - g * HG) * H, heads = min(H, p.G - h0);
-    const int n = length(seq, false);
-    const int* pages = table + static_cast<long long>(seq) * table_stride;
-    Decoder<T, D, I8, NT> dec;
-    TileRegs<T, D, I8> tr;
-    int window = t0, page = -1;                              // a lane holds the page of tile window + lane
-    auto fetch_pages = [&](int t) {
-      window = t;
-      page = -1;
-      if (t + lane < t1) {
-        page = pages[(t + lane) >> (p.ps_log2 - 4)];
-        if (page < 0 || page >= p.n_pages) { page = -1; pool_refuse(ws); }
-      }
-    };
-    auto row_of = [&](int t) -> long long {
-      if (t - window >= 32) fetch_pages(t);
-      const int pg = __shfl_sync(0xffffffffu, page, t - window);
-      return pg < 0 ? -1 : ((static_cast<long long>(pg) * p.Hkv + g) << p.ps_log2) + ((t << 4) & ((1 << p.ps_log2) - 1));
-    };
-    fetch_pages(t0);
+  int stage = 0;
+  while (cur.left > 0) {
+    const int seq = cur.seq, tiles = cur.tiles, t0 = cur.t, t1 = min(tiles, t0 + cur.left);
+    const int g = cur.g, h0 = cur.hg * H, heads = min(H, p.G - h0);
+    const int hh = g * HG + cur.hg;
+    Dec dec;
     dec.begin(q + seq * q_stride + static_cast<long long>(g * p.G + h0) * D, heads, p.scale_log2);
-    auto append = [&](int t, long long row) {                // the token's own row (every head group writes the same bytes)
-      if (k_new && t == tiles - 1) {
-        const int piece = lane % LANES;
-        const long long src = seq * kv_stride + static_cast<long long>(g) * D + piece * Piece<T>::N;
-        const long long to = lane < LANES && row >= 0 ? row + ((n - 1) & 15) : -1;
-        put_row<T, D, I8>(blob, reinterpret_cast<float*>(blob + p.ks_off), to, piece, *reinterpret_cast<const uint4*>(k_new + src));
-        put_row<T, D, I8>(blob + p.v_off, reinterpret_cast<float*>(blob + p.vs_off), to, piece, *reinterpret_cast<const uint4*>(v_new + src));
-        __syncwarp();
+#pragma unroll 1
+    for (int t = t0; t < t1;) {
+      cp_async_wait<AHEAD - U>();
+      __syncwarp();                                          // (what this lane reads other lanes have copied)
+      const int next = stage + 1 == NS ? 0 : stage + 1;
+      load_next();                                           // into the stages of the tiles before
+      const uint8_t* tile = ring + stage * S::STAGE;
+      const int lim = absent >> stage & 1u ? 0 : t == tiles - 1 ? last[seq] : 16;
+      bool two = false;
+      if constexpr (U == 2) {
+        two = t + 1 < t1;
+        if (two) {
+          load_next();
+          const int lim1 = absent >> next & 1u ? 0 : t + 1 == tiles - 1 ? last[seq] : 16;
+          const uint8_t* const both[2] = {tile, ring + next * S::STAGE};
+          const int lims[2] = {lim, lim1};
+          if (lim + lim1 > 0) dec.template tiles<2>(both, lims);
+          step(cur);
+        }
       }
-    };
-    long long row = row_of(t0);
-    append(t0, row);
-    dec.load_k(tr, blob, p, row);
-    dec.load_v(tr, blob, p, row);
-    for (int t = t0; t < t1; ++t) {
-      const int lim = row < 0 ? 0 : min(16, n - 16 * t);
-      float s[NT][4];
-      dec.scores(tr, s);
-      dec.weigh(tr, s, lim);
-      const bool more = t + 1 < t1;
-      if (more) {
-        row = row_of(t + 1);
-        append(t + 1, row);
-        dec.load_k(tr, blob, p, row);
+      if (!two) {
+        const uint8_t* const one[1] = {tile};
+        const int lims[1] = {lim};
+        if (lim > 0) dec.template tiles<1>(one, lims);
       }
-      dec.product(tr, s, lim);
-      if (more) dec.load_v(tr, blob, p, row);
+      t += two ? 2 : 1;
+      stage = !two ? next : next + 1 == NS ? 0 : next + 1;
+      step(cur);
     }
     dec.finish();
-    const int c = lane & 3;
     if (t0 == 0 && t1 == tiles) {
 #pragma unroll
       for (int nt = 0; nt < NT; ++nt)
@@ -743,7 +866,8 @@ __global__ void __launch_bounds__(kDecodeThreads, 1) pool_decode_kernel(const T*
     } else {
       const int slot = first_piece ? 0 : 1;
       first_piece = false;
-      float* dst = pieces + (warp * 2 + slot) * H * RS;
+      if (slot) { cp_async_wait<0>(); __syncwarp(); }        // (a second piece is the last: the ring is free)
+      float* dst = piece_at(warp * 2 + slot);
 #pragma unroll
       for (int nt = 0; nt < NT; ++nt)
 #pragma unroll
@@ -755,7 +879,6 @@ __global__ void __launch_bounds__(kDecodeThreads, 1) pool_decode_kernel(const T*
         }
       if (lane == 0) s_seg[warp][slot] = seq * HH + hh;
     }
-    x += t1 - t0;
   }
   __syncthreads();
 
@@ -774,7 +897,7 @@ __global__ void __launch_bounds__(kDecodeThreads, 1) pool_decode_kernel(const T*
     int j = i + 1;                                           // pieces [i, j), some of which may be unused
     while (j < 2 * kDecodeWarps && (seg_of[j] < 0 || seg_of[j] == seg)) ++j;
     const int sq = seg / HH, hh = seg - sq * HH, tiles = pre[sq + 1] - pre[sq];
-    const long long s0 = static_cast<long long>(pre[sq]) * HH + static_cast<long long>(hh) * tiles, s1 = s0 + tiles;
+    const int s0 = pre[sq] * HH + hh * tiles, s1 = s0 + tiles;
     const bool complete = s0 >= a && s1 <= e;
     const int heads = min(H, p.G - hh % HG * H);
     float* joint = joints + (static_cast<long long>(blockIdx.x) * 2 + (s0 >= a)) * kDecodePieceFloats;
@@ -783,10 +906,10 @@ __global__ void __launch_bounds__(kDecodeThreads, 1) pool_decode_kernel(const T*
       float m = -INFINITY, l = 0.f;
       float4 o = make_float4(0.f, 0.f, 0.f, 0.f);
       for (int k = i; k < j; ++k)
-        if (seg_of[k] == seg) m = fmaxf(m, pieces[(k * H + h) * RS + D]);
+        if (seg_of[k] == seg) m = fmaxf(m, piece_at(k)[h * RS + D]);
       for (int k = i; k < j; ++k) {
         if (seg_of[k] != seg) continue;
-        const float* src = pieces + (k * H + h) * RS;
+        const float* src = piece_at(k) + h * RS;
         const float f = src[D] == -INFINITY ? 0.f : fast_exp2(src[D] - m);
         const float4 v = *reinterpret_cast<const float4*>(src + d4 * 4);
         l = fmaf(f, src[D + 1], l);
@@ -802,7 +925,7 @@ __global__ void __launch_bounds__(kDecodeThreads, 1) pool_decode_kernel(const T*
     i = j;
     if (complete) continue;
     // A segment of several CTAs: the one that comes last joins them all, in their order.
-    const int c0 = static_cast<int>(s0 / per), c1 = static_cast<int>((s1 - 1) / per);
+    const int c0 = s0 / per, c1 = (s1 - 1) / per;
     __threadfence();
     __syncthreads();
     if (threadIdx.x == 0) {

@@ -78,6 +78,7 @@ extern "C" int kvc_pool_create(const kvc_pool_config* cfg, kvc_pool** out) {
   if (cfg->device < 0 || cfg->device >= kMaxDevices || cfg->flags) return KVC_EINVAL;
   const double bytes = 2.0 * cfg->n_pages * cfg->n_kv_heads * cfg->page_size * cfg->head_dim * 4;
   if (bytes > (double)(1ll << 46)) return KVC_EINVAL;
+  if ((double)cfg->n_pages * cfg->n_kv_heads * cfg->page_size >= 4294967296.0) return KVC_EINVAL;   // rows are counted in 32 bits
 
   kvc_pool* c = new (std::nothrow) kvc_pool();
   if (!c) return KVC_EINVAL;
@@ -99,7 +100,7 @@ extern "C" int kvc_pool_create(const kvc_pool_config* cfg, kvc_pool** out) {
   c->ws_clear = align_up(kvc::kWsHeaderBytes + segments * 4, 256);
   g.joints_off = (long long)c->ws_clear;
   c->ws_bytes = c->ws_clear + (size_t)kvc::kDecodeMaxCtas * 2 * kvc::kDecodePieceFloats * 4;
-  g.min_tiles = 2 * kvc::kDecodeWarps;
+  g.min_tiles = 16;
   c->launches = 0;
   c->encode = nullptr;
   c->err[0] = 0;
@@ -227,7 +228,7 @@ extern "C" int kvc_pool_decode(kvc_pool* c, const void* q, long long q_stride, c
   if (n_seqs == 0) return KVC_OK;
   // every (sequence, kv-head, head group) may be as long as the table
   const long long most = (long long)n_seqs * cf.n_kv_heads * ((c->geom.G + 7) / 8) * ((((long long)table_stride << c->geom.ps_log2) + 15) / 16);
-  if (most > 0x7fffffffll) return fail(c, KVC_EINVAL, "%d sequences of up to %d pages: 2^31 tiles of work or more", n_seqs, table_stride);
+  if (most > 0x3fffffffll) return fail(c, KVC_EINVAL, "%d sequences of up to %d pages: 2^30 tiles of work or more", n_seqs, table_stride);
   const cudaError_t e = by_shape(c, [&](auto t, auto d, auto i8) {
     using T = decltype(t);
     constexpr int D = decltype(d)::value;
@@ -235,11 +236,13 @@ extern "C" int kvc_pool_decode(kvc_pool* c, const void* q, long long q_stride, c
     auto go = [&](auto nt) {
       constexpr int NT = decltype(nt)::value;
       auto kernel = kvc::pool_decode_kernel<T, D, I8, NT>;
-      const int base = kvc::kDecodeWarps * 2 * 8 * NT * kvc::decode_row(D) * 4, smem = base + (n_seqs + 1) * 4;
+      using S = kvc::DecodeShape<T, D, I8>;
+      constexpr int W = S::template warps<NT>(), base = W * S::template warp_bytes<NT>();
+      const int smem = base + (n_seqs + 1) * 4 + n_seqs;
       static bool attr_set[kMaxDevices] = {};
-      if (cudaError_t x = opt_in_smem(kernel, base + (kvc::kDecodeMaxSeqs + 1) * 4, attr_set, cf.device)) return x;
+      if (cudaError_t x = opt_in_smem(kernel, base + (kvc::kDecodeMaxSeqs + 1) * 4 + kvc::kDecodeMaxSeqs, attr_set, cf.device)) return x;
       const int ctas = (int)std::max<long long>(1, std::min<long long>(kvc::kNumSMs, (most + c->geom.min_tiles - 1) / c->geom.min_tiles));
-      kernel<<<ctas, kvc::kDecodeThreads, smem, (cudaStream_t)stream>>>((const T*)q, q_stride, (const T*)k_new, (const T*)v_new, kv_stride, table,
+      kernel<<<ctas, W * 32, smem, (cudaStream_t)stream>>>((const T*)q, q_stride, (const T*)k_new, (const T*)v_new, kv_stride, table,
                                                                         table_stride, lens, n_seqs, (char*)blob, (char*)workspace, (T*)out, lse, c->geom);
       return cudaGetLastError();
     };

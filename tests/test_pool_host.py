@@ -23,7 +23,7 @@ def test_create_validates_configuration():
     assert rc == KVC_OK and h.value and lib.kvc_pool_launch_count(h) == 0 and isinstance(lib.kvc_pool_last_error(h), bytes)
     assert lib.kvc_pool_destroy(h) == KVC_OK
     for bad in (dict(n_q_heads=7), dict(n_q_heads=0), dict(n_kv_heads=0), dict(n_q_heads=258), dict(head_dim=96), dict(dtype=2), dict(page_format=2),
-                dict(page_size=8), dict(page_size=48), dict(page_size=512), dict(page_size=0), dict(n_pages=0), dict(max_seqs=0), dict(max_seqs=1 << 16), dict(max_seqs=4097),
+                dict(page_size=8), dict(page_size=48), dict(page_size=512), dict(page_size=0), dict(n_pages=0), dict(max_seqs=0), dict(max_seqs=1 << 16), dict(max_seqs=1025),
                 dict(softmax_scale=-1.0), dict(softmax_scale=float("nan")), dict(softmax_scale=float("inf")), dict(device=-1), dict(device=64),
                 dict(flags=1), dict(n_pages=2 ** 31 - 1, n_kv_heads=64, n_q_heads=64)):
         rc, h = create(**bad)
