@@ -12,7 +12,7 @@ struct PoolGeom {
   int Hq, Hkv, G, n_pages;
   int ps_log2;                     // page size = 1 << ps_log2
   float scale_log2;                // softmax scale times log2(e)
-  int min_tiles;                   // decode: fewest tiles of 16 keys that a CTA gets
+  int min_keys;                    // decode: fewest keys (of all segments) that a CTA gets, in whole tiles
   long long v_off, ks_off, vs_off; // byte offsets inside a blob of V, K scales, V scales (K is at 0)
   long long joints_off;            // byte offset in the workspace of the pieces of segments that span CTAs
 };
@@ -234,18 +234,21 @@ struct DecodeShape {
   static constexpr int QP = I8 && sizeof(T) == 4 ? 2 : 1;   // parts of a query or probability
   static constexpr int KS = F32 ? D / 8 : D / 16;           // steps of the contraction over channels
   // tiles on their way per warp: what registers have room for
-  static constexpr int KB = 16 * ROWB;                      // bytes of a tile's keys, and of its values
-  static constexpr int STAGE = 2 * KB + (I8 ? 128 : 0);     // ... with the scales of both
   static constexpr int OWN = I8 ? 2 * D + 16 : 0;           // the token's own row in codes, on its way to the lanes
+  // Keys of a tile: two times sixteen where registers and shared memory have room for it, so that one half's instructions fill the other's
+  // waits and the way from tile to tile is walked half as often.
+  template <int N> static __host__ __device__ constexpr int keys() { return N == 2 || (F32 && D == 128) ? 16 : 32; }
+  template <int N> static __host__ __device__ constexpr int stage() { return keys<N>() * (2 * ROWB + (I8 ? 8 : 0)); }   // K, V, scales of both
   template <int N> static __host__ __device__ constexpr int piece() { return 8 * N * (D + 4) * 4; }
-  template <int N> static __host__ __device__ constexpr int warps() { return F32 && D == 128 ? 5 : N == 2 || I8 ? 8 : 6; }
-  template <int N> static __host__ __device__ constexpr int stages() {
-    const int n = (kDecodeSmem / warps<N>() / 128 * 128 - piece<N>() - OWN) / STAGE;
-    return n < 8 ? n : 8;
+  template <int N> static __host__ __device__ constexpr int warps() {
+    return F32 && D == 128 ? 5 : N == 2 ? 8 : I8 ? 8 : D == 128 ? 6 : F32 ? 6 : 8;
   }
-  // tiles that are computed together: two where the ring then still holds the next two
-  template <int N> static __host__ __device__ constexpr int unit() { return N == 1 && stages<N>() >= 4 ? 2 : 1; }
-  template <int N> static __host__ __device__ constexpr int warp_bytes() { return (stages<N>() * STAGE + OWN + piece<N>() + 127) / 128 * 128; }
+  template <int N> static __host__ __device__ constexpr int near() { return 98304 / stage<N>(); }
+  template <int N> static __host__ __device__ constexpr int stages() {
+    const int n = (kDecodeSmem / warps<N>() / 128 * 128 - piece<N>() - OWN) / stage<N>();
+    return n < 6 ? n : 6;
+  }
+  template <int N> static __host__ __device__ constexpr int warp_bytes() { return (stages<N>() * stage<N>() + OWN + piece<N>() + 127) / 128 * 128; }
 };
 static constexpr int kDecodeMaxCtas = kNumSMs * 2;
 __host__ __device__ constexpr int decode_row(int D) { return D + 4; }    // floats of a head's row of a piece: O, m, l
@@ -314,8 +317,9 @@ template <typename T, int D, bool I8, int NT>
 struct Decoder {
   using S = DecodeShape<T, D, I8>;
   static constexpr int QR = S::KS * 2 * S::QP;
+  static constexpr int TK = S::template keys<NT>(), U = TK / 16, HB = 16 * S::ROWB, VO = TK * S::ROWB, SO = 2 * VO;   // halves, values, scales of a stage
   uint32_t qf[NT][QR];
-  float hf[NT][2];                 // 8 bits: 2^e * scale of heads 2c, 2c + 1
+  float hf[NT][2], qb[NT][2];      // 8 bits: factor of heads 2c, 2c + 1, and what their biased codes bring in (128 times the query's sum)
   float acc[NT][S::MT][4], m[NT][2], m2[NT][2], l[NT][2];
 
   static __device__ __forceinline__ int v_row(int c, int i) { return S::F32 ? c + 4 * i : 2 * c + (i & 1) + 8 * (i >> 1); }
@@ -359,11 +363,19 @@ struct Decoder {
             qf[n][2 * k + i] = hi;
             if constexpr (S::QP == 2) qf[n][2 * S::KS + 2 * k + i] = pack_f16x2(a - f16_lo(hi), b - f16_hi(hi));
           }
+        float sum = 0.f;
+        if constexpr (S::QP == 1) {
+#pragma unroll
+          for (int k = 0; k < 2 * S::KS; ++k) sum += f16_lo(qf[n][k]) + f16_hi(qf[n][k]);
+          sum += __shfl_xor_sync(0xffffffffu, sum, 1);
+          sum += __shfl_xor_sync(0xffffffffu, sum, 2);
+        }
         // the factor of heads 2c, 2c + 1 stands with the lanes of row r = head
 #pragma unroll
         for (int i = 0; i < 2; ++i) {
           const int eh = __shfl_sync(0xffffffffu, e, (2 * c + i) * 4);
-          hf[n][i] = ldexpf(scale_log2, eh);
+          hf[n][i] = ldexpf(scale_log2, S::QP == 1 ? eh + 24 : eh);
+          qb[n][i] = __shfl_sync(0xffffffffu, sum, (2 * c + i) * 4) * 0x1p-17f;
         }
       }
 #pragma unroll
@@ -386,18 +398,18 @@ struct Decoder {
     return (row * S::ROWB + byte) ^ (((row >> 1) & 3) << 5);
   }
 
-  // The sixteen rows of a tile are one stretch of its page: lane l copies pieces l, l + 32, ...
-  // kb, vb, sb: this lane's first piece of the tile in the pages.  lim: how many of the tile's rows count (the others become zeros);
+  // Sixteen rows of a tile (its half h) are one stretch of their page: lane l copies pieces l, l + 32, ...
+  // kb, vb, sb: this lane's first piece of them in the pages.  lim: how many of the rows count (the others become zeros);
   // own: which of them is the token's own (16: none), at k_own, v_own in plain pages, in `codes` (K, V, their scales) in 8 bits.
   template <bool WHOLE>
-  static __device__ __forceinline__ void load(uint8_t* stage, const char* kb, const char* vb, const char* sb, int lim, int own,
+  static __device__ __forceinline__ void load(uint8_t* stage, int h, const char* kb, const char* vb, const char* sb, int lim, int own,
                                               const char* k_own, const char* v_own, const uint8_t* codes) {
     const int lane = threadIdx.x & 31;
     const uint32_t to = smem_u32(stage);
     constexpr int PR = S::ROWB / 16, RPI = 32 / PR;          // pieces of a row, rows per copy of the warp
 #pragma unroll
-    for (int m = 0; m < S::KB / 512; ++m) {
-      const int row = m * RPI + lane / PR, k = lane % PR, at = key_at(row, k * 16);
+    for (int m = 0; m < HB / 512; ++m) {
+      const int row = m * RPI + lane / PR, k = lane % PR, at = h * HB + key_at(row, k * 16);
       if (WHOLE) copy16(to + at, kb + m * 512, 16);
       else if (row != own) copy16(to + at, kb + m * 512, row < lim ? 16 : 0);
       else if (!I8) copy16(to + at, k_own + k * 16, 16);
@@ -405,9 +417,9 @@ struct Decoder {
     }
     constexpr int PV = S::ROWB / S::VB, RPV = 32 / PV;
 #pragma unroll
-    for (int m = 0; m < S::KB / (32 * S::VB); ++m) {
+    for (int m = 0; m < HB / (32 * S::VB); ++m) {
       const int row = m * RPV + lane / PV, k = lane % PV;
-      const int at = S::KB + value_at(row, k * S::VB);
+      const int at = VO + h * HB + value_at(row, k * S::VB);
       const char* src = vb + m * (32 * S::VB);
       int bytes = S::VB;
       if (!WHOLE) {
@@ -421,15 +433,15 @@ struct Decoder {
       }
       if constexpr (S::VB == 16) copy16(to + at, src, bytes); else copy8(to + at, src, bytes);
     }
-    if constexpr (I8) {                                      // lanes 0 .. 15: keys' scales, 16 .. 31: values'
+    if constexpr (I8) {                                      // per half: lanes 0 .. 15 keys' scales, 16 .. 31 values'
       const int at = lane & 15;
-      if (!WHOLE && at == own) reinterpret_cast<float*>(stage + 2 * S::KB)[lane] = reinterpret_cast<const float*>(codes + 2 * D)[lane >> 4];
-      else copy4(to + 2 * S::KB + lane * 4, sb, WHOLE || at < lim ? 4 : 0);
+      if (!WHOLE && at == own) reinterpret_cast<float*>(stage + SO + h * 128)[lane] = reinterpret_cast<const float*>(codes + 2 * D)[lane >> 4];
+      else copy4(to + SO + h * 128 + lane * 4, sb, WHOLE || at < lim ? 4 : 0);
     }
   }
 
-  // S^T of a tile.  A chain of dependent matrix instructions is what a warp waits for most: steps alternate between two sums.
-  __device__ __forceinline__ void scores(const uint8_t* stage, float (&s)[NT][4]) const {
+  // S^T of sixteen keys.  A chain of dependent matrix instructions is what a warp waits for most: steps alternate between two sums.
+  __device__ __forceinline__ void scores(const uint8_t* keys, float (&s)[NT][4]) const {
     const int r = (threadIdx.x & 31) >> 2, c = threadIdx.x & 3;
     float part[2][NT][4];
 #pragma unroll
@@ -438,7 +450,7 @@ struct Decoder {
       for (int i = 0; i < 4; ++i) part[0][n][i] = part[1][n][i] = 0.f;
 #pragma unroll
     for (int j = 0; j < S::CK; ++j) {
-      const uint4 w0 = *reinterpret_cast<const uint4*>(stage + key_at(r, c * 16 + j * 64)), w1 = *reinterpret_cast<const uint4*>(stage + key_at(r + 8, c * 16 + j * 64));
+      const uint4 w0 = *reinterpret_cast<const uint4*>(keys + key_at(r, c * 16 + j * 64)), w1 = *reinterpret_cast<const uint4*>(keys + key_at(r + 8, c * 16 + j * 64));
       const uint32_t k0[4] = {w0.x, w0.y, w0.z, w0.w}, k1[4] = {w1.x, w1.y, w1.z, w1.w};
       if constexpr (!I8) {
 #pragma unroll
@@ -454,7 +466,13 @@ struct Decoder {
 #pragma unroll
         for (int w = 0; w < 4; ++w) {
           const uint32_t x0 = k0[w] ^ 0x80808080u, x1 = k1[w] ^ 0x80808080u;
-          const uint32_t a[4] = {codes_f16<0x4140>(x0), codes_f16<0x4140>(x1), codes_f16<0x4342>(x0), codes_f16<0x4342>(x1)};
+          uint32_t a[4];
+          if constexpr (S::QP == 1) {
+            // a biased code u as the bits of an fp16 is u * 2^-24: no arithmetic at all, and the bias goes with qb
+            a[0] = __byte_perm(x0, 0, 0x4140); a[1] = __byte_perm(x1, 0, 0x4140); a[2] = __byte_perm(x0, 0, 0x4342); a[3] = __byte_perm(x1, 0, 0x4342);
+          } else {
+            a[0] = codes_f16<0x4140>(x0); a[1] = codes_f16<0x4140>(x1); a[2] = codes_f16<0x4342>(x0); a[3] = codes_f16<0x4342>(x1);
+          }
 #pragma unroll
           for (int n = 0; n < NT; ++n)
 #pragma unroll
@@ -468,27 +486,30 @@ struct Decoder {
       for (int i = 0; i < 4; ++i) s[n][i] = part[0][n][i] + part[1][n][i];
   }
 
-  // U tiles: scores, weights, references, product.  lim: rows of a tile that count (of one of them at least one).
+  // The first N halves of a tile: scores, weights, references, product.  lim: rows of a half that count (of one of them at least one).
   // d = score - m (log2 units); in 8 bits the weight's logarithm is d + log2(value's scale) - m2.  (The difference first: a scale's
   // logarithm would be lost in a large score.)
-  template <int U>
-  __device__ __forceinline__ void tiles(const uint8_t* const (&stage)[U], const int (&lim)[U]) {
+  template <int N>
+  __device__ __forceinline__ void tile(const uint8_t* stage, const int (&lim)[2]) {
     const int lane = threadIdx.x & 31, r = lane >> 2, c = lane & 3;
     constexpr float kGrow = 8.f, kRoom = 7.f;
-    float x[U][NT][4], y[U][NT][4], lv[U][2], top = -INFINITY, top2 = -INFINITY;
+    float x[N][NT][4], y[N][NT][4], lv[N][2], top = -INFINITY, top2 = -INFINITY;
 #pragma unroll
-    for (int t = 0; t < U; ++t) {
-      scores(stage[t], x[t]);
+    for (int t = 0; t < N; ++t) {
+      scores(stage + t * HB, x[t]);
       float ks[2] = {1.f, 1.f};                              // scales of rows r and r + 8
       if constexpr (I8) {
-        const float* scales = reinterpret_cast<const float*>(stage[t] + 2 * S::KB);
+        const float* scales = reinterpret_cast<const float*>(stage + SO + t * 128);
 #pragma unroll
         for (int i = 0; i < 2; ++i) { ks[i] = scales[r + 8 * i]; lv[t][i] = __log2f(scales[16 + r + 8 * i]); }
       }
 #pragma unroll
       for (int n = 0; n < NT; ++n)
 #pragma unroll
-        for (int i = 0; i < 4; ++i) x[t][n][i] *= I8 ? hf[n][i & 1] * ks[i >> 1] : hf[n][i & 1];
+        for (int i = 0; i < 4; ++i) {
+          if constexpr (I8 && S::QP == 1) x[t][n][i] -= qb[n][i & 1];
+          x[t][n][i] *= I8 ? hf[n][i & 1] * ks[i >> 1] : hf[n][i & 1];
+        }
       if (__builtin_expect(lim[t] < 16, 0)) {                // behind the end: nothing, whatever the zeros there gave
 #pragma unroll
         for (int n = 0; n < NT; ++n)
@@ -498,7 +519,7 @@ struct Decoder {
       }
     }
 #pragma unroll
-    for (int t = 0; t < U; ++t)
+    for (int t = 0; t < N; ++t)
 #pragma unroll
       for (int n = 0; n < NT; ++n)
 #pragma unroll
@@ -515,7 +536,7 @@ struct Decoder {
         for (int i = 0; i < 2; ++i) {
           float a = -INFINITY, b = -INFINITY;
 #pragma unroll
-          for (int t = 0; t < U; ++t) a = fmaxf(a, fmaxf(x[t][n][i], x[t][n][i + 2]));
+          for (int t = 0; t < N; ++t) a = fmaxf(a, fmaxf(x[t][n][i], x[t][n][i + 2]));
 #pragma unroll
           for (int o = 4; o < 32; o <<= 1) a = fmaxf(a, __shfl_xor_sync(0xffffffffu, a, o));
           // (scores of -inf alone: a reference below all others, not -inf, so that the differences are numbers)
@@ -525,14 +546,14 @@ struct Decoder {
           float fo = f;
           if constexpr (I8) {
 #pragma unroll
-            for (int t = 0; t < U; ++t) b = fmaxf(b, fmaxf((x[t][n][i] - mn) + lv[t][0], (x[t][n][i + 2] - mn) + lv[t][1]));
+            for (int t = 0; t < N; ++t) b = fmaxf(b, fmaxf((x[t][n][i] - mn) + lv[t][0], (x[t][n][i + 2] - mn) + lv[t][1]));
 #pragma unroll
             for (int o = 4; o < 32; o <<= 1) b = fmaxf(b, __shfl_xor_sync(0xffffffffu, b, o));
             const float was = m2[n][i] + shift, mn2 = fmaxf(fmaxf(was, b), -1e30f);
             fo = fast_exp2(was - mn2);
             m2[n][i] = mn2;
 #pragma unroll
-            for (int t = 0; t < U; ++t)
+            for (int t = 0; t < N; ++t)
 #pragma unroll
               for (int k = 0; k < 2; ++k) y[t][n][i + 2 * k] = (x[t][n][i + 2 * k] - mn) + lv[t][k] - mn2;
           }
@@ -541,7 +562,7 @@ struct Decoder {
         }
     }
 #pragma unroll
-    for (int t = 0; t < U; ++t) {
+    for (int t = 0; t < N; ++t) {
 #pragma unroll
       for (int n = 0; n < NT; ++n)
 #pragma unroll
@@ -550,12 +571,12 @@ struct Decoder {
           l[n][i & 1] += e;
           x[t][n][i] = I8 ? fast_exp2(y[t][n][i] + kRoom) : e;
         }
-      product(stage[t], x[t]);
+      product(stage + VO + t * HB, x[t]);
     }
     (void)c;
   }
 
-  __device__ __forceinline__ void product(const uint8_t* stage, const float (&s)[NT][4]) {
+  __device__ __forceinline__ void product(const uint8_t* values, const float (&s)[NT][4]) {
     const int lane = threadIdx.x & 31, r = lane >> 2, c = lane & 3;
     (void)r; (void)c;
     // weights: keys on the rows -> keys side by side
@@ -588,10 +609,10 @@ struct Decoder {
 #pragma unroll
       for (int i = 0; i < 4; ++i) {
         if constexpr (S::VB == 16) {
-          const uint4 x = *reinterpret_cast<const uint4*>(stage + S::KB + value_at(v_row(c, i), r * 16 + j * 128));
+          const uint4 x = *reinterpret_cast<const uint4*>(values + value_at(v_row(c, i), r * 16 + j * 128));
           w[i][0] = x.x; w[i][1] = x.y; w[i][2] = x.z; w[i][3] = x.w;
         } else {
-          const uint2 x = *reinterpret_cast<const uint2*>(stage + S::KB + value_at(v_row(c, i), r * 8));
+          const uint2 x = *reinterpret_cast<const uint2*>(values + value_at(v_row(c, i), r * 8));
           w[i][0] = x.x; w[i][1] = x.y;
         }
       }
@@ -666,19 +687,19 @@ __global__ void __launch_bounds__(DecodeShape<T, D, I8>::template warps<NT>() * 
                                                                      float* __restrict__ lse, PoolGeom p) {
   using S = DecodeShape<T, D, I8>;
   using Dec = Decoder<T, D, I8, NT>;
-  constexpr int H = 8 * NT, RS = decode_row(D), LANES = D / Piece<T>::N, NS = S::template stages<NT>(), U = S::template unit<NT>(), AHEAD = NS - U,
+  constexpr int H = 8 * NT, RS = decode_row(D), LANES = D / Piece<T>::N, NS = S::template stages<NT>(), STAGE = S::template stage<NT>(), TK = Dec::TK,
                 WB = S::template warp_bytes<NT>();
   constexpr int kDecodeWarps = S::template warps<NT>(), kDecodeThreads = kDecodeWarps * 32;
-  static_assert(NS >= 2 && NS * S::STAGE >= S::template piece<NT>(), "two tiles on their way; the last piece overlays the ring");
+  static_assert(NS >= 2 && NS * STAGE >= S::template piece<NT>(), "two tiles on their way; the last piece overlays the ring");
   extern __shared__ __align__(128) uint8_t smem_b[];          // per warp: ring, own row, first piece; then the line of work
   int* pre = reinterpret_cast<int*>(smem_b + kDecodeWarps * WB);           // [n_seqs + 1] tiles of one head before a sequence
   uint8_t* last = reinterpret_cast<uint8_t*>(pre + n_seqs + 1);            // [n_seqs] rows of a sequence's last tile
   __shared__ int s_seg[kDecodeWarps][2], s_scan[kDecodeWarps], s_last;
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
   uint8_t* ring = smem_b + warp * WB;
-  uint8_t* own_codes = ring + NS * S::STAGE;
+  uint8_t* own_codes = ring + NS * STAGE;
   // piece 0 of warp w behind its ring, piece 1 over the ring
-  auto piece_at = [&](int i) { return reinterpret_cast<float*>(smem_b + (i >> 1) * WB + ((i & 1) ? 0 : NS * S::STAGE + S::OWN)); };
+  auto piece_at = [&](int i) { return reinterpret_cast<float*>(smem_b + (i >> 1) * WB + ((i & 1) ? 0 : NS * STAGE + S::OWN)); };
   const int HG = (p.G + H - 1) / H, HH = p.Hkv * HG;
   int* counters = reinterpret_cast<int*>(ws + kWsHeaderBytes);
   float* joints = reinterpret_cast<float*>(ws + p.joints_off);
@@ -695,8 +716,8 @@ __global__ void __launch_bounds__(DecodeShape<T, D, I8>::template warps<NT>() * 
       int len = lens[i];
       if (len < 0 || len > room) { if (blockIdx.x == 0) pool_refuse(ws); len = len < 0 ? 0 : room; }
       if (k_new) ++len;                                      // rows of the sequence, its new one included
-      x = (len + 15) >> 4;
-      last[i] = static_cast<uint8_t>((len - 1) & 15) + 1;
+      x = (len + TK - 1) / TK;
+      last[i] = static_cast<uint8_t>((len - 1) & (TK - 1)) + 1;
     }
 #pragma unroll
     for (int o = 1; o < 32; o <<= 1) { const int y = __shfl_up_sync(0xffffffffu, x, o); if (lane >= o) x += y; }
@@ -708,8 +729,23 @@ __global__ void __launch_bounds__(DecodeShape<T, D, I8>::template warps<NT>() * 
     __syncthreads();
   }
   const int total = sum * HH;
-  const int per = max((total + static_cast<int>(gridDim.x) - 1) / static_cast<int>(gridDim.x), p.min_tiles);
-  const int a = min(per * static_cast<int>(blockIdx.x), total), e = min(a + per, total);
+  const int per = max((total + static_cast<int>(gridDim.x) - 1) / static_cast<int>(gridDim.x), p.min_keys / TK);
+  // Where the ranges are short, a boundary moves to an end of its segment that is near: joining pieces across CTAs costs as much time
+  // as the loads of kNear tiles.
+  constexpr int kNear = S::template near<NT>();
+  const int near = per <= 4 * kNear ? kNear : 0;
+  auto sequence_of = [&](int x) {                            // the sequence that holds tile x: the last whose tiles begin at or before it
+    int lo = 0, hi = n_seqs;
+    while (hi - lo > 1) { const int mid = (lo + hi) >> 1; if (pre[mid] * HH <= x) lo = mid; else hi = mid; }
+    return lo;
+  };
+  auto boundary = [&](int cta) {
+    const int x = min(per * cta, total);
+    if (x == 0 || x == total || near == 0) return x;
+    const int sq = sequence_of(x), tiles = pre[sq + 1] - pre[sq], before = (x - pre[sq] * HH) % tiles, behind = tiles - before;
+    return min(before, behind) > near ? x : before <= behind ? x - before : x + behind;
+  };
+  const int a = boundary(blockIdx.x), e = boundary(blockIdx.x + 1);
 
   // sequences without a row
   for (int i = blockIdx.x; i < n_seqs; i += gridDim.x)
@@ -723,9 +759,8 @@ __global__ void __launch_bounds__(DecodeShape<T, D, I8>::template warps<NT>() * 
   const int x0 = a + (e - a) * warp / kDecodeWarps, x1 = a + (e - a) * (warp + 1) / kDecodeWarps;
   struct Cursor { int left, seq, g, hg, t, tiles; };         // tile t of kv-head g, head group hg of a sequence; how many are left from it on
   Cursor cur{x1 - x0, 0, 0, 0, 0, 0};
-  if (x0 < x1) {                                             // the sequence that holds tile x0: the last whose tiles begin at or before it
-    int hi = n_seqs;
-    while (hi - cur.seq > 1) { const int mid = (cur.seq + hi) >> 1; if (pre[mid] * HH <= x0) cur.seq = mid; else hi = mid; }
+  if (x0 < x1) {
+    cur.seq = sequence_of(x0);
     cur.tiles = pre[cur.seq + 1] - pre[cur.seq];
     const int rel = x0 - pre[cur.seq] * HH;
     const int hh = rel / cur.tiles;
@@ -743,11 +778,12 @@ __global__ void __launch_bounds__(DecodeShape<T, D, I8>::template warps<NT>() * 
     x.g = 0;
     if (x.left > 0) { do { ++x.seq; x.tiles = pre[x.seq + 1] - pre[x.seq]; } while (x.tiles == 0); }
   };
-  // loads run AHEAD tiles ahead
+  // loads run NS - 1 tiles ahead
   Cursor ld = cur;
-  uint32_t absent = 0;                                       // stages whose tile has no page
-  int ld_stage = 0, win_seq = -1, win = 0, page = -1;        // a lane holds the page of tile win + lane of sequence win_seq
+  uint32_t absent = 0;                                       // two bits per stage: the half has no page
+  int ld_stage = 0, win_seq = -1, win = 0, page = -1, page2 = -1;   // a lane holds the pages of both halves of tile win + lane of sequence win_seq
   const int c = lane & 3, page_rows = 1 << p.ps_log2;
+  const bool two_pages = TK > page_rows;
   const char* k_lane = blob + lane * 16;
   const char* v_lane = blob + p.v_off + lane * S::VB;
   const char* s_lane = blob + (lane < 16 ? p.ks_off : p.vs_off) + (lane & 15) * 4;
@@ -755,7 +791,11 @@ __global__ void __launch_bounds__(DecodeShape<T, D, I8>::template warps<NT>() * 
     if (ld.left <= 0) return;
     if (ld.seq != win_seq || static_cast<unsigned>(ld.t - win) >= 32u) {
       win_seq = ld.seq; win = ld.t;
-      page = win + lane < ld.tiles ? table[static_cast<long long>(win_seq) * table_stride + ((win + lane) >> (p.ps_log2 - 4))] : 0;
+      const int* pages = table + static_cast<long long>(win_seq) * table_stride;
+      const int t = win + lane;
+      page = t < ld.tiles ? pages[(t * TK) >> p.ps_log2] : 0;
+      page2 = page;
+      if (two_pages && (t < ld.tiles - 1 || (t == ld.tiles - 1 && last[win_seq] > 16))) page2 = pages[(t * TK + 16) >> p.ps_log2];
     }
     if (ld.t == 0 || ld.left == x1 - x0) {                   // a segment's query
       const int h0 = ld.hg * H, lines = (min(H, p.G - h0) * D * static_cast<int>(sizeof(T)) + 127) / 128;
@@ -765,38 +805,47 @@ __global__ void __launch_bounds__(DecodeShape<T, D, I8>::template warps<NT>() * 
   };
   auto load_next = [&]() {
     if (ld.left > 0) {
-      const int pg = __shfl_sync(0xffffffffu, page, ld.t - win);
-      uint8_t* stage = ring + ld_stage * S::STAGE;
+      uint8_t* stage = ring + ld_stage * STAGE;
+      const int pg = __shfl_sync(0xffffffffu, page, ld.t - win), pg2 = two_pages ? __shfl_sync(0xffffffffu, page2, ld.t - win) : pg;
+      const bool end = ld.t == ld.tiles - 1, ok = static_cast<unsigned>(pg) < static_cast<unsigned>(p.n_pages), ok2 = static_cast<unsigned>(pg2) < static_cast<unsigned>(p.n_pages);
       // (rows of a blob are fewer than 2^32)
-      const uint32_t row = ((static_cast<uint32_t>(pg) * p.Hkv + ld.g) << p.ps_log2) + ((ld.t << 4) & (page_rows - 1));
-      const bool end = ld.t == ld.tiles - 1, none = static_cast<unsigned>(pg) >= static_cast<unsigned>(p.n_pages);
-      if (__builtin_expect(!end && !none, 1)) {
-        Dec::template load<true>(stage, k_lane + static_cast<unsigned long long>(row) * S::ROWB, v_lane + static_cast<unsigned long long>(row) * S::ROWB,
-                                 s_lane + static_cast<unsigned long long>(row) * 4, 16, 16, nullptr, nullptr, nullptr);
-        absent &= ~(1u << ld_stage);
+      const uint32_t row = ((static_cast<uint32_t>(pg) * p.Hkv + ld.g) << p.ps_log2) + ((ld.t * TK) & (page_rows - 1));
+      const uint32_t row2 = two_pages ? (static_cast<uint32_t>(pg2) * p.Hkv + ld.g) << p.ps_log2 : row + 16;
+      absent &= ~(3u << (2 * ld_stage));
+      if (__builtin_expect(!end && ok && ok2, 1)) {
+#pragma unroll
+        for (int h = 0; h < TK / 16; ++h) {
+          const unsigned long long at = h ? row2 : row;
+          Dec::template load<true>(stage, h, k_lane + at * S::ROWB, v_lane + at * S::ROWB, s_lane + at * 4, 16, 16, nullptr, nullptr, nullptr);
+        }
       } else {
-        const unsigned long long at = none ? 0 : row;
-        const int lim = none ? 0 : end ? last[ld.seq] : 16;
-        int own = 16;
+        const int rows = end ? last[ld.seq] : TK;
+        if (!(ok && ok2) && lane == 0) pool_refuse(ws);
+        int own = TK;
         const char* k_own = nullptr;
         const char* v_own = nullptr;
-        if (none && lane == 0) pool_refuse(ws);
-        absent = (absent & ~(1u << ld_stage)) | static_cast<uint32_t>(none) << ld_stage;
-        if (k_new && end && !none) {                         // (every head group writes the same bytes)
-          own = lim - 1;
+        if (k_new && end && (rows > 16 ? ok2 : ok)) {        // (every head group writes the same bytes)
+          own = rows - 1;
           const long long src = ld.seq * kv_stride + static_cast<long long>(ld.g) * D;
           k_own = reinterpret_cast<const char*>(k_new + src);
           v_own = reinterpret_cast<const char*>(v_new + src);
           const int piece = lane % LANES;
-          const long long to = lane < LANES ? static_cast<long long>(row) + own : -1;
+          const long long to = lane >= LANES ? -1ll : own < 16 ? static_cast<long long>(row) + own : static_cast<long long>(row2) + own - 16;
           const uint4 kr = reinterpret_cast<const uint4*>(k_own)[piece], vr = reinterpret_cast<const uint4*>(v_own)[piece];
           float* sc = reinterpret_cast<float*>(own_codes + 2 * D);
           put_row<T, D, I8>(blob, reinterpret_cast<float*>(blob + p.ks_off), to, piece, kr, own_codes, sc);
           put_row<T, D, I8>(blob + p.v_off, reinterpret_cast<float*>(blob + p.vs_off), to, piece, vr, own_codes + D, sc + 1);
           __syncwarp();
         }
-        Dec::template load<false>(stage, k_lane + at * S::ROWB, v_lane + at * S::ROWB, s_lane + at * 4, lim, own, k_own, v_own, own_codes);
-        if (I8 && own < 16) __syncwarp();                    // (the next own row may be written over this one)
+#pragma unroll 1
+        for (int h = 0; h < TK / 16; ++h) {
+          const bool there = h ? ok2 : ok;
+          const unsigned long long at = !there ? 0 : h ? row2 : row;
+          const int lim = there ? min(16, rows - 16 * h) : 0, mine = own >> 4 == h ? own & 15 : 16;
+          absent |= static_cast<uint32_t>(!there) << (2 * ld_stage + h);
+          Dec::template load<false>(stage, h, k_lane + at * S::ROWB, v_lane + at * S::ROWB, s_lane + at * 4, lim, mine, k_own, v_own, own_codes);
+        }
+        if (I8 && own < TK) __syncwarp();                    // (the next own row may be written over this one)
       }
       if (++ld_stage == NS) ld_stage = 0;
       step(ld);
@@ -806,7 +855,7 @@ __global__ void __launch_bounds__(DecodeShape<T, D, I8>::template warps<NT>() * 
   };
   look();
 #pragma unroll 1
-  for (int i = 0; i < AHEAD; ++i) load_next();
+  for (int i = 0; i < NS - 1; ++i) load_next();
   bool first_piece = true;
   int stage = 0;
   while (cur.left > 0) {
@@ -816,34 +865,27 @@ __global__ void __launch_bounds__(DecodeShape<T, D, I8>::template warps<NT>() * 
     Dec dec;
     dec.begin(q + seq * q_stride + static_cast<long long>(g * p.G + h0) * D, heads, p.scale_log2);
 #pragma unroll 1
-    for (int t = t0; t < t1;) {
-      cp_async_wait<AHEAD - U>();
+    for (int t = t0; t < t1; ++t) {
+      cp_async_wait<NS - 2>();
       __syncwarp();                                          // (what this lane reads other lanes have copied)
-      const int next = stage + 1 == NS ? 0 : stage + 1;
-      load_next();                                           // into the stages of the tiles before
-      const uint8_t* tile = ring + stage * S::STAGE;
-      const int lim = absent >> stage & 1u ? 0 : t == tiles - 1 ? last[seq] : 16;
-      bool two = false;
-      if constexpr (U == 2) {
-        two = t + 1 < t1;
-        if (two) {
-          load_next();
-          const int lim1 = absent >> next & 1u ? 0 : t + 1 == tiles - 1 ? last[seq] : 16;
-          const uint8_t* const both[2] = {tile, ring + next * S::STAGE};
-          const int lims[2] = {lim, lim1};
-          if (lim + lim1 > 0) dec.template tiles<2>(both, lims);
-          step(cur);
-        }
+      load_next();                                           // into the stage of the tile before
+      const uint8_t* tile = ring + stage * STAGE;
+      int lim[2] = {16, 16};
+      const uint32_t none = absent >> (2 * stage) & 3u;
+      if (__builtin_expect(none || t == tiles - 1, 0)) {
+        const int rows = t == tiles - 1 ? last[seq] : TK;
+        lim[0] = none & 1u ? 0 : min(16, rows);
+        lim[1] = TK == 16 || (none & 2u) ? 0 : max(0, rows - 16);
+        if (lim[1] > 0) { if constexpr (TK == 32) dec.template tile<2>(tile, lim); }
+        else if (lim[0] > 0) dec.template tile<1>(tile, lim);
+      } else {
+        dec.template tile<TK / 16>(tile, lim);
       }
-      if (!two) {
-        const uint8_t* const one[1] = {tile};
-        const int lims[1] = {lim};
-        if (lim > 0) dec.template tiles<1>(one, lims);
-      }
-      t += two ? 2 : 1;
-      stage = !two ? next : next + 1 == NS ? 0 : next + 1;
-      step(cur);
+      if (++stage == NS) stage = 0;
     }
+    cur.left -= t1 - t0 - 1;
+    cur.t = t1 - 1;
+    step(cur);
     dec.finish();
     if (t0 == 0 && t1 == tiles) {
 #pragma unroll
@@ -925,7 +967,8 @@ __global__ void __launch_bounds__(DecodeShape<T, D, I8>::template warps<NT>() * 
     i = j;
     if (complete) continue;
     // A segment of several CTAs: the one that comes last joins them all, in their order.
-    const int c0 = s0 / per, c1 = (s1 - 1) / per;
+    // (boundaries c0 + 1 .. c1 lie inside the segment and have stayed there)
+    const int c0 = (s0 + near + per) / per - 1, c1 = (s1 - near - 1) / per;
     __threadfence();
     __syncthreads();
     if (threadIdx.x == 0) {

@@ -100,7 +100,7 @@ extern "C" int kvc_pool_create(const kvc_pool_config* cfg, kvc_pool** out) {
   c->ws_clear = align_up(kvc::kWsHeaderBytes + segments * 4, 256);
   g.joints_off = (long long)c->ws_clear;
   c->ws_bytes = c->ws_clear + (size_t)kvc::kDecodeMaxCtas * 2 * kvc::kDecodePieceFloats * 4;
-  g.min_tiles = 16;
+  g.min_keys = 256;
   c->launches = 0;
   c->encode = nullptr;
   c->err[0] = 0;
@@ -241,7 +241,7 @@ extern "C" int kvc_pool_decode(kvc_pool* c, const void* q, long long q_stride, c
       const int smem = base + (n_seqs + 1) * 4 + n_seqs;
       static bool attr_set[kMaxDevices] = {};
       if (cudaError_t x = opt_in_smem(kernel, base + (kvc::kDecodeMaxSeqs + 1) * 4 + kvc::kDecodeMaxSeqs, attr_set, cf.device)) return x;
-      const int ctas = (int)std::max<long long>(1, std::min<long long>(kvc::kNumSMs, (most + c->geom.min_tiles - 1) / c->geom.min_tiles));
+      const int ctas = (int)std::max<long long>(1, std::min<long long>(kvc::kNumSMs, (most + c->geom.min_keys / 16 - 1) / (c->geom.min_keys / 16)));
       kernel<<<ctas, W * 32, smem, (cudaStream_t)stream>>>((const T*)q, q_stride, (const T*)k_new, (const T*)v_new, kv_stride, table,
                                                                         table_stride, lens, n_seqs, (char*)blob, (char*)workspace, (T*)out, lse, c->geom);
       return cudaGetLastError();
