@@ -1,10 +1,11 @@
-"""Builds libkvc.so (the C-ABI CUDA library) in-tree with nvcc for sm_100a."""
+"""Builds in-tree libkvc.so (the C-ABI CUDA library, nvcc for sm_100a) and _pool_calls (the page pool's marshalling for Python, g++)."""
 from __future__ import annotations
 
 import os
 import shutil
 import subprocess
 import sys
+import sysconfig
 
 HERE = os.path.dirname(os.path.abspath(__file__))
 CSRC = os.path.join(HERE, "csrc")
@@ -13,18 +14,21 @@ SOURCES = ["kvc_api.cu", "pool_api.cu"]
 HEADERS = ["geom.cuh", "ptx.cuh", "kernels_cc.cuh", "kernels_tc.cuh", "compress.cuh", "pool.cuh"]
 
 
-def _stale() -> bool:
-    if not os.path.exists(LIB):
+CALLS = os.path.join(HERE, "_pool_calls" + (sysconfig.get_config_var("EXT_SUFFIX") or ".so"))
+
+
+def _stale(target: str, sources) -> bool:
+    if not os.path.exists(target):
         return True
-    t = os.path.getmtime(LIB)
-    deps = [os.path.join(CSRC, f) for f in SOURCES + HEADERS]
+    t = os.path.getmtime(target)
+    deps = [os.path.join(CSRC, f) for f in sources]
     deps.append(os.path.join(os.path.dirname(HERE), "include", "kvc.h"))
     return any(os.path.getmtime(d) > t for d in deps if os.path.exists(d))
 
 
 def build(force: bool = False, verbose: bool = False) -> str:
     """Compile the library if it is missing or older than its sources; returns its path."""
-    if not force and not _stale():
+    if not force and not _stale(LIB, SOURCES + HEADERS):
         return LIB
     nvcc = os.environ.get("NVCC", "/usr/local/cuda/bin/nvcc")
     if not os.path.exists(nvcc):
@@ -49,5 +53,31 @@ def build(force: bool = False, verbose: bool = False) -> str:
     return LIB
 
 
+def build_calls(force: bool = False) -> str:
+    """Compile _pool_calls if it is missing or older than its source; returns its path."""
+    if not force and not _stale(CALLS, ["pool_calls.cpp"]):
+        return CALLS
+    gxx = os.environ.get("CXX") or shutil.which("g++")
+    if not gxx:
+        if os.path.exists(CALLS):
+            return CALLS                                  # no compiler here: use the module as shipped
+        raise RuntimeError("_pool_calls is missing and g++ was not found")
+    import torch
+    from torch.utils.cpp_extension import include_paths, library_paths
+    cuda = os.environ.get("CUDA_HOME", "/usr/local/cuda")
+    tmp = CALLS + f".tmp{os.getpid()}"
+    cmd = [gxx, "-O2", "-std=c++17", "-shared", "-fPIC", "-fvisibility=hidden", "-w", f"-D_GLIBCXX_USE_CXX11_ABI={int(torch.compiled_with_cxx11_abi())}"]
+    cmd += [f"-I{p}" for p in include_paths() + [os.path.join(cuda, "include"), sysconfig.get_paths()["include"]]]
+    cmd += [os.path.join(CSRC, "pool_calls.cpp"), "-o", tmp] + [f"-L{p}" for p in library_paths()]
+    cmd += ["-ltorch_python", "-ltorch_cpu", "-lc10_cuda", "-lc10"]
+    r = subprocess.run(cmd, capture_output=True, text=True)
+    if r.returncode != 0:
+        sys.stderr.write(r.stdout + r.stderr)
+        raise RuntimeError("g++ failed building _pool_calls")
+    os.replace(tmp, CALLS)
+    return CALLS
+
+
 if __name__ == "__main__":
     print(build(force="--force" in sys.argv, verbose="-v" in sys.argv))
+    print(build_calls(force="--force" in sys.argv))

@@ -42,9 +42,12 @@ __device__ __forceinline__ RowScale row_scale(uint32_t top) {
   if (top >= 0x7f800000u) { r.s = __uint_as_float(0x7fffffffu); r.inv = 0.f; }   // an infinity or a NaN: the row reads back as NaN
   return r;
 }
-__device__ __forceinline__ uint32_t row_code(float x, float inv) {
-  // |x * inv| can reach 127 and a rounding, never 127.5 (an infinity or NaN times inv = 0 converts to 0)
-  return static_cast<uint32_t>(__float2int_rn(__fmul_rn(x, inv))) & 0xffu;
+// rint(x * inv) in the lowest byte: |x * inv| can reach 127 and a rounding, never 127.5, and the sum with 1.5 * 2^23 is rounded to
+// whole numbers, to even at ties (a conversion instruction takes four times as long).
+__device__ __forceinline__ uint32_t row_code(float x, float inv) { return __float_as_uint(__fadd_rn(__fmul_rn(x, inv), 12582912.f)); }
+__device__ __forceinline__ uint32_t row_codes(const float* x, float inv) {
+  const uint32_t lo = __byte_perm(row_code(x[0], inv), row_code(x[1], inv), 0x0040), hi = __byte_perm(row_code(x[2], inv), row_code(x[3], inv), 0x0040);
+  return __byte_perm(lo, hi, 0x5410);
 }
 
 // The values of a 16-byte piece of a row.
@@ -89,8 +92,7 @@ __device__ __forceinline__ void put_row(char* codes, float* scales, long long ds
     const RowScale rs = row_scale(top);
     uint32_t c[N / 4];
 #pragma unroll
-    for (int i = 0; i < N / 4; ++i)
-      c[i] = row_code(x[4 * i], rs.inv) | row_code(x[4 * i + 1], rs.inv) << 8 | row_code(x[4 * i + 2], rs.inv) << 16 | row_code(x[4 * i + 3], rs.inv) << 24;
+    for (int i = 0; i < N / 4; ++i) c[i] = row_codes(x + 4 * i, rs.inv);
     if (own_codes) {                                         // (kvc_pool_decode: the row is wanted at once)
       if constexpr (N == 8) *reinterpret_cast<uint2*>(own_codes + piece * 8) = make_uint2(c[0], c[1]);
       else *reinterpret_cast<uint32_t*>(own_codes + piece * 4) = c[0];
@@ -107,7 +109,10 @@ __device__ __forceinline__ void put_row(char* codes, float* scales, long long ds
 // ------------------------------------------------------------------------------------------------
 // Rows -> pages.  A row of 16-byte pieces is held by D * sizeof(T) / 16 lanes, K and V of kRowsPerThread rows in flight per thread.
 // Bound: HBM.  grid ceil(n * Hkv / rows per block), block 256.
-static constexpr int kPoolThreads = 256, kRowsPerThread = 2;
+#ifndef KRPT
+#define KRPT 2
+#endif
+static constexpr int kPoolThreads = 256, kRowsPerThread = KRPT;
 template <typename T, int D> __host__ __device__ constexpr int pool_rows_per_block() { return kPoolThreads / (D / Piece<T>::N) * kRowsPerThread; }
 
 template <typename T, int D, bool I8>
@@ -153,7 +158,8 @@ __device__ __forceinline__ uint4 get_piece(const char* codes, const float* scale
     const float s = scales[src];
     float x[N];
 #pragma unroll
-    for (int i = 0; i < N; ++i) x[i] = s * static_cast<float>(static_cast<int>(c[i / 4] << (24 - 8 * (i % 4))) >> 24);
+    for (int i = 0; i < N; ++i)                              // 2^23 + 128 + c as bits, less 2^23 + 128: exact
+      x[i] = s * (__uint_as_float(__byte_perm(c[i / 4] ^ 0x80808080u, 0x4B000000u, 0x7440 + i % 4)) - 8388736.f);
     return Piece<T>::pack(x);
   }
 }

@@ -1,0 +1,244 @@
+// The page pool's per-call marshalling for Python: checks of tensors, outputs, pointers and the current stream, then the C ABI.
+// (Through ctypes a decode call took 13 us of host time -- two allocations 3.9, the checks 2.5, converting 15 arguments
+// and the launch 4.5 -- more than the kernel takes on the GPU for a small batch.)
+// The C ABI's functions come as addresses from the library that pool.py has loaded; nothing is linked against it.
+#include <torch/csrc/autograd/python_variable.h>
+#include <ATen/ATen.h>
+#include <c10/cuda/CUDAStream.h>
+
+#include <string>
+
+#include "../../include/kvc.h"
+
+namespace {
+
+struct Calls {
+  kvc_pool* pool;
+  decltype(&kvc_pool_write) write;
+  decltype(&kvc_pool_read) read;
+  decltype(&kvc_pool_decode) decode;
+  decltype(&kvc_pool_prompt) prompt;
+  int64_t hq, hkv, d;
+  at::ScalarType dtype;
+  int device;
+  void* ws;
+  int64_t blob_bytes;
+};
+
+struct Bad { std::string text; };                            // -> ValueError
+
+std::string describe(const at::Tensor& t) {
+  std::string s = std::string(c10::toString(t.scalar_type())) + " [";
+  for (int64_t i = 0; i < t.dim(); ++i) s += (i ? ", " : "") + std::to_string(t.size(i));
+  s += "] with strides [";
+  for (int64_t i = 0; i < t.dim(); ++i) s += (i ? ", " : "") + std::to_string(t.stride(i));
+  return s + "] on " + t.device().str();
+}
+
+const at::Tensor& tensor(PyObject* o, const char* name) {
+  if (!THPVariable_Check(o)) throw Bad{std::string(name) + ": a tensor is wanted, got " + Py_TYPE(o)->tp_name};
+  return THPVariable_Unpack(o);
+}
+bool here(const Calls* c, const at::Tensor& t) { return t.is_cuda() && t.get_device() == c->device; }
+
+// Rows [n][heads][d] of the pool's dtype; the strides of the first two dimensions are free.
+const at::Tensor& rows(const Calls* c, PyObject* o, const char* name, int64_t n, int64_t heads) {
+  const at::Tensor& t = tensor(o, name);
+  if (t.dim() != 3 || t.size(0) != n || t.size(1) != heads || t.size(2) != c->d || t.scalar_type() != c->dtype || !here(c, t) || (t.stride(2) != 1 && t.numel()))
+    throw Bad{std::string(name) + ": " + c10::toString(c->dtype) + " rows [" + std::to_string(n) + ", " + std::to_string(heads) + ", " + std::to_string(c->d) +
+              "] on cuda:" + std::to_string(c->device) + ", innermost contiguous; got " + describe(t)};
+  return t;
+}
+// The same with a token's heads side by side: the stride of a token's rows, in elements.
+int64_t token_stride(const Calls* c, const at::Tensor& t, const char* name) {
+  if (t.size(1) > 1 && t.stride(1) != c->d && t.numel()) throw Bad{std::string(name) + ": the heads of a token must be contiguous; got " + describe(t)};
+  return t.size(0) > 1 ? t.stride(0) : std::max<int64_t>(t.stride(0), t.size(1) * c->d);
+}
+// Strides (token, kv-head) of two row tensors, which must agree; dimensions of one element may say anything.
+void pair_strides(const Calls* c, const at::Tensor& k, const at::Tensor& v, int64_t* ts, int64_t* hs) {
+  const int64_t n = k.size(0);
+  if ((n > 1 && k.stride(0) != v.stride(0)) || (c->hkv > 1 && n > 0 && k.stride(1) != v.stride(1)))
+    throw Bad{"k and v must have the same strides; got " + describe(k) + " and " + describe(v)};
+  *ts = n > 1 ? k.stride(0) : c->d;
+  *hs = c->hkv > 1 && n > 0 ? k.stride(1) : c->d;
+}
+const at::Tensor& index(const Calls* c, PyObject* o, const char* name, at::ScalarType type) {
+  const at::Tensor& t = tensor(o, name);
+  if (t.scalar_type() != type || !here(c, t) || !t.is_contiguous())
+    throw Bad{std::string(name) + ": a contiguous " + c10::toString(type) + " tensor on cuda:" + std::to_string(c->device) + "; got " + describe(t)};
+  return t;
+}
+at::Tensor output(const Calls* c, PyObject* o, int64_t n, const at::Tensor& like) {
+  if (o == Py_None) return at::empty({n, c->hq, c->d}, like.options());
+  const at::Tensor& t = rows(c, o, "out", n, c->hq);
+  if (!t.is_contiguous()) throw Bad{"out must be contiguous; got " + describe(t)};
+  return t;
+}
+at::Tensor lse_of(const Calls* c, PyObject* o, int64_t n, const at::Tensor& like) {
+  if (o == Py_None) return at::empty({n, c->hq}, like.options().dtype(at::kFloat));
+  const at::Tensor& t = index(c, o, "lse", at::kFloat);
+  if (t.dim() != 2 || t.size(0) != n || t.size(1) != c->hq)
+    throw Bad{"lse: [" + std::to_string(n) + ", " + std::to_string(c->hq) + "]; got " + describe(t)};
+  return t;
+}
+char* layer_of(const Calls* c, PyObject* blob, PyObject* layer) {
+  const at::Tensor& t = tensor(blob, "blob");
+  if (t.dim() != 2 || !here(c, t) || t.stride(1) != 1 || t.size(1) * t.element_size() < c->blob_bytes)
+    throw Bad{"blob: [layers, " + std::to_string(c->blob_bytes) + "] bytes on cuda:" + std::to_string(c->device) + "; got " + describe(t)};
+  const long l = PyLong_AsLong(layer);
+  if (l == -1 && PyErr_Occurred()) throw python_error();
+  if (l < 0 || l >= t.size(0)) {
+    PyErr_Format(PyExc_IndexError, "layer %ld outside [0, %lld)", l, (long long)t.size(0));
+    python_error e;
+    e.persist();
+    throw e;
+  }
+  return static_cast<char*>(t.data_ptr()) + l * t.stride(0) * t.element_size();
+}
+void* stream_of(const Calls* c) { return c10::cuda::getCurrentCUDAStream(static_cast<c10::DeviceIndex>(c->device)).stream(); }
+
+PyObject* result(int rc) {                                   // None, or the C ABI's status
+  if (rc != KVC_OK) return PyLong_FromLong(rc);
+  Py_RETURN_NONE;
+}
+PyObject* result(int rc, at::Tensor a, at::Tensor b) {
+  if (rc != KVC_OK) return PyLong_FromLong(rc);
+  PyObject* x = THPVariable_Wrap(std::move(a));
+  PyObject* y = x ? THPVariable_Wrap(std::move(b)) : nullptr;
+  PyObject* r = y ? PyTuple_Pack(2, x, y) : nullptr;
+  Py_XDECREF(x);
+  Py_XDECREF(y);
+  return r;
+}
+
+template <typename F>
+PyObject* guarded(PyObject* const* args, Py_ssize_t n, Py_ssize_t want, F f) {
+  if (n != want) { PyErr_Format(PyExc_TypeError, "%zd arguments are wanted, got %zd", want, n); return nullptr; }
+  const Calls* c = static_cast<const Calls*>(PyCapsule_GetPointer(args[0], "kvc_pool_calls"));
+  if (!c) return nullptr;
+  try {
+    return f(c);
+  } catch (const Bad& e) {
+    PyErr_SetString(PyExc_ValueError, e.text.c_str());
+  } catch (python_error& e) {
+    e.restore();
+  } catch (const std::exception& e) {
+    PyErr_SetString(PyExc_RuntimeError, e.what());
+  }
+  return nullptr;
+}
+
+// write(calls, blob, layer, k, v, slots)
+PyObject* do_write(PyObject*, PyObject* const* a, Py_ssize_t na) {
+  return guarded(a, na, 6, [&](const Calls* c) {
+    const at::Tensor& slots = index(c, a[5], "slots", at::kLong);
+    if (slots.dim() != 1) throw Bad{"slots: one dimension; got " + describe(slots)};
+    const int64_t n = slots.size(0);
+    const at::Tensor &k = rows(c, a[3], "k", n, c->hkv), &v = rows(c, a[4], "v", n, c->hkv);
+    int64_t ts, hs;
+    pair_strides(c, k, v, &ts, &hs);
+    char* blob = layer_of(c, a[1], a[2]);
+    return result(c->write(c->pool, k.data_ptr(), v.data_ptr(), ts, hs, reinterpret_cast<const long long*>(slots.data_ptr<int64_t>()), n, blob, c->ws, stream_of(c)));
+  });
+}
+
+// read(calls, blob, layer, slots, k or None, v or None) -> (k, v)
+PyObject* do_read(PyObject*, PyObject* const* a, Py_ssize_t na) {
+  return guarded(a, na, 6, [&](const Calls* c) {
+    const at::Tensor& slots = index(c, a[3], "slots", at::kLong);
+    if (slots.dim() != 1) throw Bad{"slots: one dimension; got " + describe(slots)};
+    const int64_t n = slots.size(0);
+    if ((a[4] == Py_None) != (a[5] == Py_None)) throw Bad{"k and v go together"};
+    const bool make = a[4] == Py_None;
+    at::Tensor k = make ? at::empty({n, c->hkv, c->d}, slots.options().dtype(c->dtype)) : rows(c, a[4], "k", n, c->hkv);
+    at::Tensor v = make ? at::empty({n, c->hkv, c->d}, slots.options().dtype(c->dtype)) : rows(c, a[5], "v", n, c->hkv);
+    int64_t ts, hs;
+    pair_strides(c, k, v, &ts, &hs);
+    char* blob = layer_of(c, a[1], a[2]);
+    const int rc = c->read(c->pool, blob, reinterpret_cast<const long long*>(slots.data_ptr<int64_t>()), n, k.data_ptr(), v.data_ptr(), ts, hs, c->ws, stream_of(c));
+    return result(rc, std::move(k), std::move(v));
+  });
+}
+
+// decode(calls, blob, layer, q, table, lens, k or None, v or None, out or None, lse or None) -> (out, lse)
+PyObject* do_decode(PyObject*, PyObject* const* a, Py_ssize_t na) {
+  return guarded(a, na, 10, [&](const Calls* c) {
+    const at::Tensor& q0 = tensor(a[3], "q");
+    if (q0.dim() != 3) throw Bad{"q: three dimensions; got " + describe(q0)};
+    const int64_t n = q0.size(0);
+    const at::Tensor& q = rows(c, a[3], "q", n, c->hq);
+    const at::Tensor &table = index(c, a[4], "table", at::kInt), &lens = index(c, a[5], "lens", at::kInt);
+    if (table.dim() != 2 || table.size(0) != n || lens.dim() != 1 || lens.size(0) != n || table.size(1) > 0x7fffffff || n > 0x7fffffff)
+      throw Bad{"table [" + std::to_string(n) + ", pages] and lens [" + std::to_string(n) + "]; got " + describe(table) + " and " + describe(lens)};
+    if ((a[6] == Py_None) != (a[7] == Py_None)) throw Bad{"k and v go together"};
+    const void *kp = nullptr, *vp = nullptr;
+    int64_t kv_stride = 0;
+    if (a[6] != Py_None) {
+      const at::Tensor &k = rows(c, a[6], "k", n, c->hkv), &v = rows(c, a[7], "v", n, c->hkv);
+      kv_stride = token_stride(c, k, "k");
+      if (token_stride(c, v, "v") != kv_stride) throw Bad{"k and v must have the same strides; got " + describe(k) + " and " + describe(v)};
+      kp = k.data_ptr();
+      vp = v.data_ptr();
+    }
+    const int64_t q_stride = token_stride(c, q, "q");
+    char* blob = layer_of(c, a[1], a[2]);
+    at::Tensor out = output(c, a[8], n, q), lse = lse_of(c, a[9], n, q);
+    const int rc = c->decode(c->pool, q.data_ptr(), q_stride, kp, vp, kv_stride, table.data_ptr<int>(), static_cast<int>(table.size(1)), lens.data_ptr<int>(),
+                             static_cast<int>(n), blob, c->ws, out.data_ptr(), lse.data_ptr<float>(), stream_of(c));
+    return result(rc, std::move(out), std::move(lse));
+  });
+}
+
+// prompt(calls, q, k, v, address of the kvc_prompt_plan, items, out or None, lse or None) -> (out, lse)
+PyObject* do_prompt(PyObject*, PyObject* const* a, Py_ssize_t na) {
+  return guarded(a, na, 8, [&](const Calls* c) {
+    const kvc_prompt_plan* plan = static_cast<const kvc_prompt_plan*>(PyLong_AsVoidPtr(a[4]));
+    if (!plan) throw Bad{"a plan is wanted"};
+    const int64_t n = plan->n_tokens;
+    const at::Tensor &q = rows(c, a[1], "q", n, c->hq), &k = rows(c, a[2], "k", n, c->hkv), &v = rows(c, a[3], "v", n, c->hkv);
+    const int64_t q_stride = token_stride(c, q, "q"), kv_stride = token_stride(c, k, "k");
+    if (token_stride(c, v, "v") != kv_stride) throw Bad{"k and v must have the same strides; got " + describe(k) + " and " + describe(v)};
+    const at::Tensor& items = index(c, a[5], "items", at::kByte);
+    if (static_cast<size_t>(items.numel()) < plan->item_bytes) throw Bad{"items: the plan's; got " + describe(items)};
+    at::Tensor out = output(c, a[6], n, q), lse = lse_of(c, a[7], n, q);
+    const int rc = c->prompt(c->pool, q.data_ptr(), q_stride, k.data_ptr(), v.data_ptr(), kv_stride, plan, items.data_ptr(), c->ws, out.data_ptr(),
+                             lse.data_ptr<float>(), stream_of(c));
+    return result(rc, std::move(out), std::move(lse));
+  });
+}
+
+// calls(pool, write, read, decode, prompt, hq, hkv, d, bf16, device, ws, blob bytes): addresses and numbers
+PyObject* do_calls(PyObject*, PyObject* args) {
+  unsigned long long pool, w, r, dec, pro, ws;
+  long long hq, hkv, d, blob_bytes;
+  int bf16, device;
+  if (!PyArg_ParseTuple(args, "KKKKKLLLpiKL", &pool, &w, &r, &dec, &pro, &hq, &hkv, &d, &bf16, &device, &ws, &blob_bytes)) return nullptr;
+  Calls* c = new (std::nothrow) Calls();
+  if (!c) return PyErr_NoMemory();
+  c->pool = reinterpret_cast<kvc_pool*>(pool);
+  c->write = reinterpret_cast<decltype(c->write)>(w);
+  c->read = reinterpret_cast<decltype(c->read)>(r);
+  c->decode = reinterpret_cast<decltype(c->decode)>(dec);
+  c->prompt = reinterpret_cast<decltype(c->prompt)>(pro);
+  c->hq = hq; c->hkv = hkv; c->d = d;
+  c->dtype = bf16 ? at::kBFloat16 : at::kFloat;
+  c->device = device;
+  c->ws = reinterpret_cast<void*>(ws);
+  c->blob_bytes = blob_bytes;
+  PyObject* cap = PyCapsule_New(c, "kvc_pool_calls", [](PyObject* o) { delete static_cast<Calls*>(PyCapsule_GetPointer(o, "kvc_pool_calls")); });
+  if (!cap) delete c;
+  return cap;
+}
+
+PyMethodDef methods[] = {
+    {"calls", do_calls, METH_VARARGS, nullptr},
+    {"write", reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(do_write)), METH_FASTCALL, nullptr},
+    {"read", reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(do_read)), METH_FASTCALL, nullptr},
+    {"decode", reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(do_decode)), METH_FASTCALL, nullptr},
+    {"prompt", reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(do_prompt)), METH_FASTCALL, nullptr},
+    {nullptr, nullptr, 0, nullptr}};
+PyModuleDef module = {PyModuleDef_HEAD_INIT, "_pool_calls", nullptr, -1, methods, nullptr, nullptr, nullptr, nullptr};
+
+}  // namespace
+
+PyMODINIT_FUNC PyInit__pool_calls() { return PyModule_Create(&module); }

@@ -156,7 +156,7 @@ def test_rows_into_pages_and_back(dtype, fmt, hkv, d, page, n, layout):
 
 def before_parts(pool, blob):
     other = Pool.__new__(Pool)
-    other.__dict__.update({k: v for k, v in pool.__dict__.items() if k != "_h"})
+    other.__dict__.update({k: v for k, v in pool.__dict__.items() if k not in ("_h", "_calls")})
     other.blob = blob
     return other.pages(0)
 
@@ -518,3 +518,11 @@ def test_refusals():
     with pytest.raises(ValueError):
         Pool(4, 2, 64, BF16, 4, 16, blob=torch.zeros(1, 100, dtype=torch.uint8, device="cuda"))
     assert pool.launch_count() == 0 and pool.status() == KVC_OK
+    keep, pool.blob = pool.blob, pool.blob[:, :-256]
+    with pytest.raises(ValueError):
+        pool.write(0, x, x, slots)
+    pool.blob = keep
+    pool.close()
+    for call in (lambda: pool.write(0, x, x, slots), lambda: pool.read(0, slots), lambda: pool.decode(0, q, table, lens), lambda: pool.prompt(q, x, x, plan)):
+        with pytest.raises(ValueError):
+            call()
