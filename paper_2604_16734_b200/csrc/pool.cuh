@@ -21,11 +21,12 @@ static constexpr int kPoolInvalid = -1;   // KVC_EINVAL in the status word: a sl
 
 __device__ __forceinline__ void pool_refuse(char* ws) { atomicExch(reinterpret_cast<int*>(ws), kPoolInvalid); }
 
-// Row (page, kv-head, row of the page) of a pool, or -1 for a slot outside it.
-__device__ __forceinline__ long long pool_row(const PoolGeom& p, long long slot, int head) {
-  const long long page = slot >> p.ps_log2;
-  if (slot < 0 || page >= p.n_pages) return -1;
-  return ((page * p.Hkv + head) << p.ps_log2) + (slot & ((1 << p.ps_log2) - 1));
+// Row (page, kv-head, row of the page) of a blob, or kNoRow for a slot outside the pool.  (A blob has fewer than 2^32 - 1 rows.)
+static constexpr uint32_t kNoRow = 0xffffffffu;
+__device__ __forceinline__ uint32_t pool_row(const PoolGeom& p, long long slot, int head) {
+  const unsigned long long page = static_cast<unsigned long long>(slot) >> p.ps_log2;
+  if (page >= static_cast<unsigned long long>(p.n_pages)) return kNoRow;      // (a negative slot among them)
+  return ((static_cast<uint32_t>(page) * p.Hkv + head) << p.ps_log2) + (static_cast<uint32_t>(slot) & ((1u << p.ps_log2) - 1));
 }
 
 // ------------------------------------------------------------------------------------------------
@@ -107,95 +108,153 @@ __device__ __forceinline__ void put_row(char* codes, float* scales, long long ds
 }
 
 // ------------------------------------------------------------------------------------------------
-// Rows -> pages.  A row of 16-byte pieces is held by D * sizeof(T) / 16 lanes, K and V of kRowsPerThread rows in flight per thread.
-// Bound: HBM.  grid ceil(n * Hkv / rows per block), block 256.
-#ifndef KRPT
-#define KRPT 2
-#endif
-static constexpr int kPoolThreads = 256, kRowsPerThread = KRPT;
-template <typename T, int D> __host__ __device__ constexpr int pool_rows_per_block() { return kPoolThreads / (D / Piece<T>::N) * kRowsPerThread; }
+// Rows -> pages and back.  A row is held by `kLanes` lanes, two 16-byte pieces each, kLanes apart; a block takes kRowTokens tokens of one
+// kv-head, so that its side of the pages is contiguous, and the kv-heads of the same tokens follow one another, so that the other
+// side is too.  K and V of two rows are in flight per thread.  Bound: HBM (65536 tokens, 8 kv-heads, d = 128, bf16 <-> 8 bits).
+static constexpr int kPoolThreads = 256, kRowsPerThread = 2;
+template <typename T, int D> struct RowShape {
+  static constexpr int N = Piece<T>::N, kLanes = D / N / 2, kRows = kPoolThreads / kLanes, kRowTokens = kRows * kRowsPerThread;
+};
 
+// What a lane has of a row (values x[2N], its two pieces) as codes in row `dst` of K or V pages.
+template <typename T, int D>
+__device__ __forceinline__ void put_codes(char* codes, float* scales, uint32_t dst, int lane_of_row, const uint4 (&raw)[2]) {
+  using R = RowShape<T, D>;
+  constexpr int N = R::N;
+  float x[2 * N];
+  Piece<T>::values(raw[0], x);
+  Piece<T>::values(raw[1], x + N);
+  uint32_t top = 0;
+#pragma unroll
+  for (int i = 0; i < 2 * N; ++i) top = max(top, __float_as_uint(x[i]) & 0x7fffffffu);
+#pragma unroll
+  for (int o = R::kLanes / 2; o > 0; o >>= 1) top = max(top, __shfl_xor_sync(0xffffffffu, top, o));
+  const RowScale rs = row_scale(top);
+  if (dst == kNoRow) return;
+  char* to = codes + static_cast<unsigned long long>(dst) * D + lane_of_row * N;
+#pragma unroll
+  for (int i = 0; i < 2; ++i) {
+    if constexpr (N == 8) *reinterpret_cast<uint2*>(to + i * R::kLanes * N) = make_uint2(row_codes(x + i * N, rs.inv), row_codes(x + i * N + 4, rs.inv));
+    else *reinterpret_cast<uint32_t*>(to + i * R::kLanes * N) = row_codes(x + i * N, rs.inv);
+  }
+  if (lane_of_row == 0) scales[dst] = rs.s;
+}
+
+// grid ceil(n / kRowTokens) * Hkv, block 256
 template <typename T, int D, bool I8>
 __global__ void __launch_bounds__(kPoolThreads) pool_write_kernel(const T* __restrict__ k, const T* __restrict__ v, long long ts,
-                                                                  long long hs, const long long* __restrict__ slots, unsigned rows,
+                                                                  long long hs, const long long* __restrict__ slots, unsigned n,
                                                                   char* __restrict__ blob, char* __restrict__ ws, PoolGeom p) {
-  constexpr int LANES = D / Piece<T>::N, RPP = kPoolThreads / LANES;
-  const int piece = threadIdx.x % LANES;
-  const unsigned row0 = blockIdx.x * (RPP * kRowsPerThread) + threadIdx.x / LANES;
-  uint4 kr[kRowsPerThread], vr[kRowsPerThread];
-  long long dst[kRowsPerThread];
+  using R = RowShape<T, D>;
+  const int l = threadIdx.x % R::kLanes;
+  const unsigned h = blockIdx.x % p.Hkv, t0 = blockIdx.x / p.Hkv * R::kRowTokens + threadIdx.x / R::kLanes;
+  const long long at = h * hs + l * R::N;
+  uint4 kr[kRowsPerThread][2], vr[kRowsPerThread][2];
+  uint32_t dst[kRowsPerThread];
 #pragma unroll
   for (int i = 0; i < kRowsPerThread; ++i) {
-    const unsigned row = row0 + i * RPP;
-    dst[i] = -1;
-    kr[i] = vr[i] = make_uint4(0, 0, 0, 0);
-    if (row < rows) {
-      const unsigned t = row / p.Hkv, h = row - t * p.Hkv;
-      const long long slot = slots[t], src = t * ts + h * hs + piece * Piece<T>::N;
+    const unsigned t = t0 + i * R::kRows;
+    dst[i] = kNoRow;
+    kr[i][0] = kr[i][1] = vr[i][0] = vr[i][1] = make_uint4(0, 0, 0, 0);
+    if (t < n) {
+      const long long slot = slots[t], src = t * ts + at;
+#pragma unroll
+      for (int j = 0; j < 2; ++j) {
+        kr[i][j] = __ldcs(reinterpret_cast<const uint4*>(k + src) + j * R::kLanes);
+        vr[i][j] = __ldcs(reinterpret_cast<const uint4*>(v + src) + j * R::kLanes);
+      }
       dst[i] = pool_row(p, slot, h);
-      if (dst[i] < 0 && slot >= 0 && piece == 0) pool_refuse(ws);
-      kr[i] = *reinterpret_cast<const uint4*>(k + src);
-      vr[i] = *reinterpret_cast<const uint4*>(v + src);
+      if (dst[i] == kNoRow && slot >= 0 && l == 0) pool_refuse(ws);
     }
   }
 #pragma unroll
   for (int i = 0; i < kRowsPerThread; ++i) {
-    put_row<T, D, I8>(blob, reinterpret_cast<float*>(blob + p.ks_off), dst[i], piece, kr[i]);
-    put_row<T, D, I8>(blob + p.v_off, reinterpret_cast<float*>(blob + p.vs_off), dst[i], piece, vr[i]);
-  }
-}
-
-// A piece of row `src` of the pages, as values of T.
-template <typename T, int D, bool I8>
-__device__ __forceinline__ uint4 get_piece(const char* codes, const float* scales, long long src, int piece) {
-  constexpr int N = Piece<T>::N, LANES = D / N;
-  if constexpr (!I8) {
-    return reinterpret_cast<const uint4*>(codes)[src * LANES + piece];
-  } else {
-    uint32_t c[2] = {0, 0};
-    if constexpr (N == 8) { const uint2 w = *reinterpret_cast<const uint2*>(codes + src * D + piece * 8); c[0] = w.x; c[1] = w.y; }
-    else c[0] = *reinterpret_cast<const uint32_t*>(codes + src * D + piece * 4);
-    const float s = scales[src];
-    float x[N];
+    if constexpr (I8) {
+      put_codes<T, D>(blob, reinterpret_cast<float*>(blob + p.ks_off), dst[i], l, kr[i]);
+      put_codes<T, D>(blob + p.v_off, reinterpret_cast<float*>(blob + p.vs_off), dst[i], l, vr[i]);
+    } else if (dst[i] != kNoRow) {
+      uint4* to = reinterpret_cast<uint4*>(blob + static_cast<unsigned long long>(dst[i]) * (D * sizeof(T))) + l;
+      uint4* vo = reinterpret_cast<uint4*>(blob + p.v_off + static_cast<unsigned long long>(dst[i]) * (D * sizeof(T))) + l;
 #pragma unroll
-    for (int i = 0; i < N; ++i)                              // 2^23 + 128 + c as bits, less 2^23 + 128: exact
-      x[i] = s * (__uint_as_float(__byte_perm(c[i / 4] ^ 0x80808080u, 0x4B000000u, 0x7440 + i % 4)) - 8388736.f);
-    return Piece<T>::pack(x);
+      for (int j = 0; j < 2; ++j) { to[j * R::kLanes] = kr[i][j]; vo[j * R::kLanes] = vr[i][j]; }
+    }
   }
 }
 
-// Pages -> rows.  Bound: HBM.  grid and block as above.
+// Codes -> values of T: 2^23 + 128 + c as bits, less 2^23 + 128, is exact.
+template <typename T>
+__device__ __forceinline__ uint4 from_codes(const uint32_t* c, float s) {
+  constexpr int N = Piece<T>::N;
+  float x[N];
+#pragma unroll
+  for (int i = 0; i < N; ++i) x[i] = s * (__uint_as_float(__byte_perm(c[i / 4] ^ 0x80808080u, 0x4B000000u, 0x7440 + i % 4)) - 8388736.f);
+  return Piece<T>::pack(x);
+}
+
+// grid and block as above
 template <typename T, int D, bool I8>
 __global__ void __launch_bounds__(kPoolThreads) pool_read_kernel(const char* __restrict__ blob, const long long* __restrict__ slots,
-                                                                 unsigned rows, T* __restrict__ k, T* __restrict__ v, long long ts,
+                                                                 unsigned n, T* __restrict__ k, T* __restrict__ v, long long ts,
                                                                  long long hs, char* __restrict__ ws, PoolGeom p) {
-  constexpr int LANES = D / Piece<T>::N, RPP = kPoolThreads / LANES;
-  const int piece = threadIdx.x % LANES;
-  const unsigned row0 = blockIdx.x * (RPP * kRowsPerThread) + threadIdx.x / LANES;
-  uint4 kr[kRowsPerThread], vr[kRowsPerThread];
+  using R = RowShape<T, D>;
+  constexpr int N = R::N, W = I8 ? N / 4 : 4;                // words of a piece in the pages
+  const int l = threadIdx.x % R::kLanes;
+  const unsigned h = blockIdx.x % p.Hkv, t0 = blockIdx.x / p.Hkv * R::kRowTokens + threadIdx.x / R::kLanes;
+  const long long at = h * hs + l * N;
+  uint32_t kr[kRowsPerThread][2][W], vr[kRowsPerThread][2][W];
+  float sk[kRowsPerThread], sv[kRowsPerThread];
 #pragma unroll
   for (int i = 0; i < kRowsPerThread; ++i) {
-    const unsigned row = row0 + i * RPP;
-    kr[i] = vr[i] = make_uint4(0, 0, 0, 0);
-    if (row < rows) {
-      const unsigned t = row / p.Hkv, h = row - t * p.Hkv;
-      const long long slot = slots[t], src = pool_row(p, slot, h);
-      if (src < 0) {
-        if (slot >= 0 && piece == 0) pool_refuse(ws);
+    const unsigned t = t0 + i * R::kRows;
+    sk[i] = sv[i] = 0.f;
+#pragma unroll
+    for (int j = 0; j < 2; ++j)
+#pragma unroll
+      for (int w = 0; w < W; ++w) kr[i][j][w] = vr[i][j][w] = 0;
+    if (t < n) {
+      const long long slot = slots[t];
+      const uint32_t src = pool_row(p, slot, h);
+      if (src == kNoRow) {
+        if (slot >= 0 && l == 0) pool_refuse(ws);
       } else {
-        kr[i] = get_piece<T, D, I8>(blob, reinterpret_cast<const float*>(blob + p.ks_off), src, piece);
-        vr[i] = get_piece<T, D, I8>(blob + p.v_off, reinterpret_cast<const float*>(blob + p.vs_off), src, piece);
+        const char* kp = blob + static_cast<unsigned long long>(src) * (D * (I8 ? 1 : sizeof(T))) + l * (W * 4);
+        const char* vp = kp + p.v_off;
+#pragma unroll
+        for (int j = 0; j < 2; ++j) {
+          if constexpr (W == 4) {
+            const uint4 a = __ldcs(reinterpret_cast<const uint4*>(kp) + j * R::kLanes), b = __ldcs(reinterpret_cast<const uint4*>(vp) + j * R::kLanes);
+            kr[i][j][0] = a.x; kr[i][j][1] = a.y; kr[i][j][2] = a.z; kr[i][j][3] = a.w;
+            vr[i][j][0] = b.x; vr[i][j][1] = b.y; vr[i][j][2] = b.z; vr[i][j][3] = b.w;
+          } else if constexpr (W == 2) {
+            const uint2 a = __ldcs(reinterpret_cast<const uint2*>(kp) + j * R::kLanes), b = __ldcs(reinterpret_cast<const uint2*>(vp) + j * R::kLanes);
+            kr[i][j][0] = a.x; kr[i][j][1] = a.y; vr[i][j][0] = b.x; vr[i][j][1] = b.y;
+          } else {
+            kr[i][j][0] = __ldcs(reinterpret_cast<const uint32_t*>(kp) + j * R::kLanes);
+            vr[i][j][0] = __ldcs(reinterpret_cast<const uint32_t*>(vp) + j * R::kLanes);
+          }
+        }
+        if constexpr (I8) {
+          sk[i] = reinterpret_cast<const float*>(blob + p.ks_off)[src];
+          sv[i] = reinterpret_cast<const float*>(blob + p.vs_off)[src];
+        }
       }
     }
   }
 #pragma unroll
   for (int i = 0; i < kRowsPerThread; ++i) {
-    const unsigned row = row0 + i * RPP;
-    if (row < rows) {
-      const unsigned t = row / p.Hkv, h = row - t * p.Hkv;
-      const long long to = t * ts + h * hs + piece * Piece<T>::N;
-      *reinterpret_cast<uint4*>(k + to) = kr[i];
-      *reinterpret_cast<uint4*>(v + to) = vr[i];
+    const unsigned t = t0 + i * R::kRows;
+    if (t >= n) continue;
+    uint4* ko = reinterpret_cast<uint4*>(k + t * ts + at);
+    uint4* vo = reinterpret_cast<uint4*>(v + t * ts + at);
+#pragma unroll
+    for (int j = 0; j < 2; ++j) {
+      if constexpr (I8) {
+        ko[j * R::kLanes] = from_codes<T>(kr[i][j], sk[i]);
+        vo[j * R::kLanes] = from_codes<T>(vr[i][j], sv[i]);
+      } else {
+        ko[j * R::kLanes] = make_uint4(kr[i][j][0], kr[i][j][1], kr[i][j][2], kr[i][j][3]);
+        vo[j * R::kLanes] = make_uint4(vr[i][j][0], vr[i][j][1], vr[i][j][2], vr[i][j][3]);
+      }
     }
   }
 }

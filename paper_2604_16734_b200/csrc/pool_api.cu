@@ -78,7 +78,7 @@ extern "C" int kvc_pool_create(const kvc_pool_config* cfg, kvc_pool** out) {
   if (cfg->device < 0 || cfg->device >= kMaxDevices || cfg->flags) return KVC_EINVAL;
   const double bytes = 2.0 * cfg->n_pages * cfg->n_kv_heads * cfg->page_size * cfg->head_dim * 4;
   if (bytes > (double)(1ll << 46)) return KVC_EINVAL;
-  if ((double)cfg->n_pages * cfg->n_kv_heads * cfg->page_size >= 4294967296.0) return KVC_EINVAL;   // rows are counted in 32 bits
+  if ((double)cfg->n_pages * cfg->n_kv_heads * cfg->page_size >= 4294967295.0) return KVC_EINVAL;   // rows are counted in 32 bits
 
   kvc_pool* c = new (std::nothrow) kvc_pool();
   if (!c) return KVC_EINVAL;
@@ -179,12 +179,12 @@ extern "C" int kvc_pool_write(kvc_pool* c, const void* k, const void* v, long lo
   if (!live(c)) return KVC_ESTATE;
   if (int rc = check_rows(c, k, v, token_stride, head_stride, slots, n, blob, workspace)) return rc;
   if (n == 0) return KVC_OK;
-  const unsigned rows = (unsigned)(n * c->cfg.n_kv_heads);
+  const kvc_pool_config& cf = c->cfg;
   const cudaError_t e = by_shape(c, [&](auto t, auto d, auto i8) {
     using T = decltype(t);
-    constexpr int D = decltype(d)::value, per = kvc::pool_rows_per_block<T, D>();
-    kvc::pool_write_kernel<T, D, decltype(i8)::value><<<(rows + per - 1) / per, kvc::kPoolThreads, 0, (cudaStream_t)stream>>>(
-        (const T*)k, (const T*)v, token_stride, head_stride, slots, rows, (char*)blob, (char*)workspace, c->geom);
+    constexpr int D = decltype(d)::value, per = kvc::RowShape<T, D>::kRowTokens;
+    kvc::pool_write_kernel<T, D, decltype(i8)::value><<<(unsigned)((n + per - 1) / per) * cf.n_kv_heads, kvc::kPoolThreads, 0, (cudaStream_t)stream>>>(
+        (const T*)k, (const T*)v, token_stride, head_stride, slots, (unsigned)n, (char*)blob, (char*)workspace, c->geom);
     return cudaGetLastError();
   });
   c->launches++;
@@ -196,12 +196,12 @@ extern "C" int kvc_pool_read(kvc_pool* c, const void* blob, const long long* slo
   if (!live(c)) return KVC_ESTATE;
   if (int rc = check_rows(c, k, v, token_stride, head_stride, slots, n, blob, workspace)) return rc;
   if (n == 0) return KVC_OK;
-  const unsigned rows = (unsigned)(n * c->cfg.n_kv_heads);
+  const kvc_pool_config& cf = c->cfg;
   const cudaError_t e = by_shape(c, [&](auto t, auto d, auto i8) {
     using T = decltype(t);
-    constexpr int D = decltype(d)::value, per = kvc::pool_rows_per_block<T, D>();
-    kvc::pool_read_kernel<T, D, decltype(i8)::value><<<(rows + per - 1) / per, kvc::kPoolThreads, 0, (cudaStream_t)stream>>>(
-        (const char*)blob, slots, rows, (T*)k, (T*)v, token_stride, head_stride, (char*)workspace, c->geom);
+    constexpr int D = decltype(d)::value, per = kvc::RowShape<T, D>::kRowTokens;
+    kvc::pool_read_kernel<T, D, decltype(i8)::value><<<(unsigned)((n + per - 1) / per) * cf.n_kv_heads, kvc::kPoolThreads, 0, (cudaStream_t)stream>>>(
+        (const char*)blob, slots, (unsigned)n, (T*)k, (T*)v, token_stride, head_stride, (char*)workspace, c->geom);
     return cudaGetLastError();
   });
   c->launches++;
