@@ -76,13 +76,7 @@ struct TcSmemAttn {
 };
 static_assert(offsetof(TcSmemAttn, kv_full) == offsetof(TcSmemAttn, q_full) + 2 * sizeof(uint64_t));   // (walked as one array)
 
-//
-// PACKED: whole prompts of different lengths, one after the other in q, k, v and out; no cache, no append, no key split.  A
-// CTA takes a piece of work from a list (`cache` points at it: first token of the prompt, its tokens, first row tile, row
-// tiles), sorted by key tiles, longest first.  Loads may run past the prompt's end into the next one's rows: its keys are
-// masked like those of later tokens, its values are zeroed in shared memory (warp 11) so that whatever they are -- infinities, NaN
-// -- does not meet a zero probability, and its rows are not written.  p.score_off is the address of the log-sum-exp rows (0: none).
-template <int D, int R, bool PACKED = false>
+template <int D, int R>
 __global__ void __launch_bounds__(kAttnThreads, 1) attn_tc_kernel(const __grid_constant__ CUtensorMap tm_q,
                                                                    const __grid_constant__ CUtensorMap tm_k,
                                                                    const __grid_constant__ CUtensorMap tm_v,
@@ -117,14 +111,8 @@ __global__ void __launch_bounds__(kAttnThreads, 1) attn_tc_kernel(const __grid_c
   // R = 1: a row tile per CTA (or per cluster).  R = 2: the first n_pairs CTAs of a kv-head take two row tiles each, the
   // others one of the rest.
   const int TOK = 128 / p.G, rows = TOK * p.G;
-  int4 item = make_int4(0, 0, 0, 0);
-  if constexpr (PACKED) {
-    item = reinterpret_cast<const int4*>(cache)[lin / gridDim.y];
-    p.n = item.y;
-  }
-  const int base = PACKED ? item.x : 0;          // the prompt's first token
-  const bool has_B = R == 2 && (PACKED ? item.w == 2 : bx < n_pairs);
-  const int tile0 = PACKED ? item.z : R == 1 ? bx / S : has_B ? 2 * bx : n_pairs + bx;
+  const bool has_B = R == 2 && bx < n_pairs;
+  const int tile0 = R == 1 ? bx / S : has_B ? 2 * bx : n_pairs + bx;
   const int tokA = tile0 * TOK, tokB = tokA + TOK, tok_end = has_B ? tokB + TOK : tokB;
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
   const int last_tok = min(tok_end, p.n) - 1;
@@ -143,8 +131,7 @@ __global__ void __launch_bounds__(kAttnThreads, 1) attn_tc_kernel(const __grid_c
 
   // block tiles [u_lo, u_hi) of this CTA that it appends to the cache (see warp 11): those that begin in its rows
   const int u_lo = max(max(t_begin - Tc, 0), (tokA + 127) / 128), u_hi = min(t_end - Tc, (tok_end + 127) / 128);
-  const bool appends = !PACKED && u_hi > u_lo;
-  const bool v_tail = PACKED && T * 128 > p.n;   // the last key tile runs past the prompt's end
+  const bool appends = u_hi > u_lo;
 
   if (threadIdx.x == 0) {
     for (int i = 0; i < 2; ++i) {
@@ -158,7 +145,6 @@ __global__ void __launch_bounds__(kAttnThreads, 1) attn_tc_kernel(const __grid_c
     mbar_init(&sh.mma_done[0], 1); mbar_init(&sh.mma_done[1], 1);
     mbar_init(&sh.comb_full, 1);
     // key split: every other rank of the cluster will copy its partial of this rank's rows here
-    // (packed prompts: the values behind the prompt's end, see warp 11)
     if (S > 1) mbar_expect_tx(&sh.comb_full, (S - 1) * (128 / S) * (D + 4) * 4);
     mbar_fence_init();
   }
@@ -199,7 +185,7 @@ __global__ void __launch_bounds__(kAttnThreads, 1) attn_tc_kernel(const __grid_c
       if (kt < Tc) {                             // cache rows kt*128 .. (rows past n_c are masked by the softmax)
         for (int sub = 0; sub < NSUB; ++sub) tma_load_4d(dst + sub * kSubTileBytes, v ? &tm_v : &tm_k, &sh.kv_full[slot], sub * 64, kt * 128, g, layer);
       } else {                                   // block tokens (kt - Tc)*128 .. (tokens past n are zero-filled)
-        for (int sub = 0; sub < NSUB; ++sub) tma_load_4d(dst + sub * kSubTileBytes, v ? &tm_vin : &tm_kin, &sh.kv_full[slot], sub * 64, g, base + (kt - Tc) * 128, layer);
+        for (int sub = 0; sub < NSUB; ++sub) tma_load_4d(dst + sub * kSubTileBytes, v ? &tm_vin : &tm_kin, &sh.kv_full[slot], sub * 64, g, (kt - Tc) * 128, layer);
       }
       return true;
     };
@@ -214,12 +200,12 @@ __global__ void __launch_bounds__(kAttnThreads, 1) attn_tc_kernel(const __grid_c
       if (Tl > 0 && lane < 2 + 2 * NSUB * min(Tl, 2)) {
         if (lane < 2) {
           if (lane == 0 || has_B)
-            for (int sub = 0; sub < NSUB; ++sub) tma_prefetch_l2_4d(&tm_q, sub * 64, g * p.G, base + (lane ? tokB : tokA), layer);
+            for (int sub = 0; sub < NSUB; ++sub) tma_prefetch_l2_4d(&tm_q, sub * 64, g * p.G, lane ? tokB : tokA, layer);
         } else {
           const int i = (lane - 2) / NSUB, sub = (lane - 2) % NSUB;      // K or V of key tile t_begin + i/2
           const int kt = t_begin + (i >> 1);
           if (kt < Tc) tma_prefetch_l2_4d((i & 1) ? &tm_v : &tm_k, sub * 64, kt * 128, g, layer);
-          else tma_prefetch_l2_4d((i & 1) ? &tm_vin : &tm_kin, sub * 64, g, base + (kt - Tc) * 128, layer);
+          else tma_prefetch_l2_4d((i & 1) ? &tm_vin : &tm_kin, sub * 64, g, (kt - Tc) * 128, layer);
         }
       }
       __syncwarp();
@@ -231,7 +217,7 @@ __global__ void __launch_bounds__(kAttnThreads, 1) attn_tc_kernel(const __grid_c
       if (lane == 0 && Tl > 0) {
         mbar_expect_tx(&sh.q_full[0], NSUB * rows * 128);
         for (int sub = 0; sub < NSUB; ++sub)
-          tma_load_4d(sQ + sub * kSubTileBytes, &tm_q, &sh.q_full[0], sub * 64, g * p.G, base + tokA, layer);
+          tma_load_4d(sQ + sub * kSubTileBytes, &tm_q, &sh.q_full[0], sub * 64, g * p.G, tokA, layer);
         // In the order in which they are needed: an SM takes in 64 bytes a cycle, and V tiles asked for beside the first K tile
         // hold it up (three key tiles: 0.5 us of a call of 8).  Behind the first fill K runs a tile ahead of V, as S does.
         const int fill = min(Tl, kSlots);
@@ -240,7 +226,7 @@ __global__ void __launch_bounds__(kAttnThreads, 1) attn_tc_kernel(const __grid_c
           if (j == 0 && has_B) {                   // (row tile A can start on Q_A and the first K tile)
             mbar_expect_tx(&sh.q_full[1], NSUB * rows * 128);
             for (int sub = 0; sub < NSUB; ++sub)
-              tma_load_4d(sQ + TILE_BYTES + sub * kSubTileBytes, &tm_q, &sh.q_full[1], sub * 64, g * p.G, base + tokB, layer);
+              tma_load_4d(sQ + TILE_BYTES + sub * kSubTileBytes, &tm_q, &sh.q_full[1], sub * 64, g * p.G, tokB, layer);
           }
           load_tile(j, 1);
         }
@@ -277,23 +263,6 @@ __global__ void __launch_bounds__(kAttnThreads, 1) attn_tc_kernel(const __grid_c
               tma_store_wait_read();
             }
             mbar_arrive(&sh.kv_empty[slot]);
-          }
-        }
-      }
-      if constexpr (PACKED) {
-        if (v_tail) {
-          // comb_full, first phase: the issuer of P V has seen the slot's tile before the last one (a parity alone does not tell
-          // which round a barrier is in); second phase: the tile is as it should be.
-          const int slot = kSlots + (Tl - 1) % kSlots, seen = p.n - (T - 1) * 128;
-          bool there = mbar_wait(&sh.comb_full, 0, abort_flag);
-          there = there && mbar_wait(&sh.kv_full[slot], ((Tl - 1) / kSlots) & 1, abort_flag);
-          if (__all_sync(0xffffffffu, there)) {
-            for (int sub = 0; sub < NSUB; ++sub)
-              for (int i = seen * 8 + lane; i < 128 * 8; i += 32)
-                reinterpret_cast<uint4*>(ring + slot * TILE_BYTES + sub * kSubTileBytes)[i] = make_uint4(0, 0, 0, 0);
-            fence_proxy_async_smem();
-            __syncwarp();
-            if (lane == 0) mbar_arrive(&sh.comb_full);
           }
         }
       }
@@ -337,13 +306,6 @@ __global__ void __launch_bounds__(kAttnThreads, 1) attn_tc_kernel(const __grid_c
         for (int i = 0; i < n_items && ok; ++i) {
           const int t = i & 1, it = i >> 1, j = has_B ? it : i, slot = j % kSlots;
           if (!has_B || t == 0) ok = mbar_wait(&sh.kv_full[kSlots + slot], (j / kSlots) & 1, abort_flag);
-          if constexpr (PACKED) {
-            // (asked once per key tile, with its first item)
-            if (v_tail && (!has_B || t == 0)) {
-              if (ok && j == max(Tl - 1 - kSlots, 0)) mbar_arrive(&sh.comb_full);
-              if (j == Tl - 1) ok = ok && mbar_wait(&sh.comb_full, 1, abort_flag);
-            }
-          }
           const uint32_t v_lo = v_lo0 + slot * (TILE_BYTES >> 4), tP = tmem + 128 + t * 64, tO = tmem + 256 + t * 128;
 #pragma unroll
           for (int half = 0; half < 2; ++half) {
@@ -396,11 +358,6 @@ __global__ void __launch_bounds__(kAttnThreads, 1) attn_tc_kernel(const __grid_c
     const int tok0 = (t && !alt) ? tokB : tokA;             // (both groups hold the rows of tile A when they alternate)
     const int tok = tok0 + r / p.G, hh = r % p.G;
     const bool row_valid = r < rows && tok < p.n;
-    const bool clip = PACKED && tok0 + TOK > p.n;           // the row tile runs past the prompt's end: its rows leave one by one
-    const long long out_row = static_cast<long long>(base + tok) * p.Hq + g * p.G + hh;
-    auto put_lse = [&](float x) {
-      if constexpr (PACKED) { if (p.score_off) reinterpret_cast<float*>(p.score_off)[out_row] = x; }
-    };
     const uint32_t lane_addr = static_cast<uint32_t>((warp & 3) * 32) << 16;
     const uint32_t tmem_S = tmem + lane_addr, tmem_P = tmem + 128 + t * 64 + lane_addr, tmem_O = tmem + 256 + t * 128 + lane_addr;
     float m_ref = -INFINITY, l = 0.f;                        // reference maximum (log2 units) and row sum
@@ -561,16 +518,10 @@ __global__ void __launch_bounds__(kAttnThreads, 1) attn_tc_kernel(const __grid_c
             vv.y = pack_bf16x2(__uint_as_float(o[8 * i + 2]) * inv, __uint_as_float(o[8 * i + 3]) * inv);
             vv.z = pack_bf16x2(__uint_as_float(o[8 * i + 4]) * inv, __uint_as_float(o[8 * i + 5]) * inv);
             vv.w = pack_bf16x2(__uint_as_float(o[8 * i + 6]) * inv, __uint_as_float(o[8 * i + 7]) * inv);
-            if (PACKED && clip) {
-              if (row_valid) reinterpret_cast<uint4*>(out + out_row * D)[c * 4 + i] = vv;
-            } else {
-              *out_chunk(t, c * 4 + i) = vv;
-            }
+            *out_chunk(t, c * 4 + i) = vv;
           }
         }
-        if constexpr (PACKED) {
-          if (row_valid) put_lse((m_ref + log2f(l)) * 0.6931471805599453f);
-        } else if (row_valid) {
+        if (row_valid) {
           float* lse = reinterpret_cast<float*>(ws_slot(ws, p, layer) + p.lse_off);
           lse[static_cast<long long>(tok) * p.Hq + head_row + hh] = (m_ref + log2f(l)) * 0.6931471805599453f;
         }
@@ -578,9 +529,9 @@ __global__ void __launch_bounds__(kAttnThreads, 1) attn_tc_kernel(const __grid_c
       }
       tmem_done();
       named_barrier(1 + 3 * t, 128);                           // (ids 1 and 4)
-      if (r == 0 && ok && !clip) {
+      if (r == 0 && ok) {
         for (int sub = 0; sub < NSUB; ++sub)
-          tma_store_4d(&tm_out, sQ + t * TILE_BYTES + sub * kSubTileBytes, sub * 64, g * p.G, base + tok0, layer);
+          tma_store_4d(&tm_out, sQ + t * TILE_BYTES + sub * kSubTileBytes, sub * 64, g * p.G, tok0, layer);
         tma_store_commit();
         tma_store_wait_read();
       }
@@ -636,7 +587,7 @@ __global__ void __launch_bounds__(kAttnThreads, 1) attn_tc_kernel(const __grid_c
               // Straight from the registers, a sector per store: no barrier, no wait for a copy to leave (requests: image
               // 2897 -> 2842 us, image from a graph 1552 -> 1514, tiled image 2831 -> 2736).
               if (row_valid) {
-                __nv_bfloat16* dst = out + layer * p.out_ls + (static_cast<long long>(base + tok) * p.Hq + head_row + hh) * D + t * H + c * 32;
+                __nv_bfloat16* dst = out + layer * p.out_ls + (static_cast<long long>(tok) * p.Hq + head_row + hh) * D + t * H + c * 32;
                 if ((reinterpret_cast<uintptr_t>(dst) & 31) == 0) {
                   st_global_v8(dst, pk);
                   st_global_v8(dst + 16, pk + 8);
@@ -645,20 +596,12 @@ __global__ void __launch_bounds__(kAttnThreads, 1) attn_tc_kernel(const __grid_c
                   for (int i = 0; i < 4; ++i) reinterpret_cast<uint4*>(dst)[i] = make_uint4(pk[4 * i], pk[4 * i + 1], pk[4 * i + 2], pk[4 * i + 3]);
                 }
               }
-            } else if (PACKED && clip) {
-              if (row_valid) {
-#pragma unroll
-                for (int i = 0; i < 4; ++i)
-                  reinterpret_cast<uint4*>(out + out_row * D + t * H + c * 32)[i] = make_uint4(pk[4 * i], pk[4 * i + 1], pk[4 * i + 2], pk[4 * i + 3]);
-              }
             } else {
 #pragma unroll
               for (int i = 0; i < 4; ++i) *out_chunk(0, t * (H / 8) + c * 4 + i) = make_uint4(pk[4 * i], pk[4 * i + 1], pk[4 * i + 2], pk[4 * i + 3]);
             }
           }
-          if constexpr (PACKED) {
-            if (row_valid && t == 0) put_lse((m_all + log2f(L)) * 0.6931471805599453f);
-          } else if (row_valid && t == 0) {
+          if (row_valid && t == 0) {
             float* lse = reinterpret_cast<float*>(ws_slot(ws, p, layer) + p.lse_off);
             lse[static_cast<long long>(tok) * p.Hq + head_row + hh] = (m_all + log2f(L)) * 0.6931471805599453f;
           }
@@ -667,9 +610,9 @@ __global__ void __launch_bounds__(kAttnThreads, 1) attn_tc_kernel(const __grid_c
         tmem_done();
         if constexpr (R == 2) {
           named_barrier(1, 256);
-          if (threadIdx.x == 0 && ok && !clip) {
+          if (threadIdx.x == 0 && ok) {
             for (int sub = 0; sub < NSUB; ++sub)
-              tma_store_4d(&tm_out, sQ + sub * kSubTileBytes, sub * 64, g * p.G, base + tok0, layer);
+              tma_store_4d(&tm_out, sQ + sub * kSubTileBytes, sub * 64, g * p.G, tok0, layer);
             tma_store_commit();
             tma_store_wait_read();
           }

@@ -108,12 +108,13 @@ __device__ __forceinline__ void put_row(char* codes, float* scales, long long ds
 }
 
 // ------------------------------------------------------------------------------------------------
-// Rows -> pages and back.  A row is held by `kLanes` lanes, two 16-byte pieces each, kLanes apart; a block takes kRowTokens tokens of one
+// Rows -> pages and back.  A row is held by `kLanes` lanes, two 16-byte pieces each, kLanes apart; a block takes tokens of one
 // kv-head, so that its side of the pages is contiguous, and the kv-heads of the same tokens follow one another, so that the other
-// side is too.  K and V of two rows are in flight per thread.  Bound: HBM (65536 tokens, 8 kv-heads, d = 128, bf16 <-> 8 bits).
-static constexpr int kPoolThreads = 256, kRowsPerThread = 2;
+// side is too.  Bound: HBM, at 5.6 - 5.7 TB/s of 6.45 for a copy (54000 tokens, 8 kv-heads, d = 128: bf16 into 8 bits 42 us with
+// two rows in flight per thread, 45 with one, 52 with four; back 41 with one, 43 with two, 52 with four).
+static constexpr int kPoolThreads = 256, kWriteRows = 2, kReadRows = 1;
 template <typename T, int D> struct RowShape {
-  static constexpr int N = Piece<T>::N, kLanes = D / N / 2, kRows = kPoolThreads / kLanes, kRowTokens = kRows * kRowsPerThread;
+  static constexpr int N = Piece<T>::N, kLanes = D / N / 2, kRows = kPoolThreads / kLanes;
 };
 
 // What a lane has of a row (values x[2N], its two pieces) as codes in row `dst` of K or V pages.
@@ -134,25 +135,25 @@ __device__ __forceinline__ void put_codes(char* codes, float* scales, uint32_t d
   char* to = codes + static_cast<unsigned long long>(dst) * D + lane_of_row * N;
 #pragma unroll
   for (int i = 0; i < 2; ++i) {
-    if constexpr (N == 8) *reinterpret_cast<uint2*>(to + i * R::kLanes * N) = make_uint2(row_codes(x + i * N, rs.inv), row_codes(x + i * N + 4, rs.inv));
+    if constexpr (N == 8) __stcs(reinterpret_cast<uint2*>(to + i * R::kLanes * N), make_uint2(row_codes(x + i * N, rs.inv), row_codes(x + i * N + 4, rs.inv)));
     else *reinterpret_cast<uint32_t*>(to + i * R::kLanes * N) = row_codes(x + i * N, rs.inv);
   }
   if (lane_of_row == 0) scales[dst] = rs.s;
 }
 
-// grid ceil(n / kRowTokens) * Hkv, block 256
+// grid ceil(n / (kRows * kWriteRows)) * Hkv, block 256
 template <typename T, int D, bool I8>
 __global__ void __launch_bounds__(kPoolThreads) pool_write_kernel(const T* __restrict__ k, const T* __restrict__ v, long long ts,
                                                                   long long hs, const long long* __restrict__ slots, unsigned n,
                                                                   char* __restrict__ blob, char* __restrict__ ws, PoolGeom p) {
   using R = RowShape<T, D>;
   const int l = threadIdx.x % R::kLanes;
-  const unsigned h = blockIdx.x % p.Hkv, t0 = blockIdx.x / p.Hkv * R::kRowTokens + threadIdx.x / R::kLanes;
+  const unsigned h = blockIdx.x % p.Hkv, t0 = blockIdx.x / p.Hkv * (R::kRows * kWriteRows) + threadIdx.x / R::kLanes;
   const long long at = h * hs + l * R::N;
-  uint4 kr[kRowsPerThread][2], vr[kRowsPerThread][2];
-  uint32_t dst[kRowsPerThread];
+  uint4 kr[kWriteRows][2], vr[kWriteRows][2];
+  uint32_t dst[kWriteRows];
 #pragma unroll
-  for (int i = 0; i < kRowsPerThread; ++i) {
+  for (int i = 0; i < kWriteRows; ++i) {
     const unsigned t = t0 + i * R::kRows;
     dst[i] = kNoRow;
     kr[i][0] = kr[i][1] = vr[i][0] = vr[i][1] = make_uint4(0, 0, 0, 0);
@@ -168,7 +169,7 @@ __global__ void __launch_bounds__(kPoolThreads) pool_write_kernel(const T* __res
     }
   }
 #pragma unroll
-  for (int i = 0; i < kRowsPerThread; ++i) {
+  for (int i = 0; i < kWriteRows; ++i) {
     if constexpr (I8) {
       put_codes<T, D>(blob, reinterpret_cast<float*>(blob + p.ks_off), dst[i], l, kr[i]);
       put_codes<T, D>(blob + p.v_off, reinterpret_cast<float*>(blob + p.vs_off), dst[i], l, vr[i]);
@@ -191,7 +192,7 @@ __device__ __forceinline__ uint4 from_codes(const uint32_t* c, float s) {
   return Piece<T>::pack(x);
 }
 
-// grid and block as above
+// grid ceil(n / (kRows * kReadRows)) * Hkv, block 256
 template <typename T, int D, bool I8>
 __global__ void __launch_bounds__(kPoolThreads) pool_read_kernel(const char* __restrict__ blob, const long long* __restrict__ slots,
                                                                  unsigned n, T* __restrict__ k, T* __restrict__ v, long long ts,
@@ -199,12 +200,12 @@ __global__ void __launch_bounds__(kPoolThreads) pool_read_kernel(const char* __r
   using R = RowShape<T, D>;
   constexpr int N = R::N, W = I8 ? N / 4 : 4;                // words of a piece in the pages
   const int l = threadIdx.x % R::kLanes;
-  const unsigned h = blockIdx.x % p.Hkv, t0 = blockIdx.x / p.Hkv * R::kRowTokens + threadIdx.x / R::kLanes;
+  const unsigned h = blockIdx.x % p.Hkv, t0 = blockIdx.x / p.Hkv * (R::kRows * kReadRows) + threadIdx.x / R::kLanes;
   const long long at = h * hs + l * N;
-  uint32_t kr[kRowsPerThread][2][W], vr[kRowsPerThread][2][W];
-  float sk[kRowsPerThread], sv[kRowsPerThread];
+  uint32_t kr[kReadRows][2][W], vr[kReadRows][2][W];
+  float sk[kReadRows], sv[kReadRows];
 #pragma unroll
-  for (int i = 0; i < kRowsPerThread; ++i) {
+  for (int i = 0; i < kReadRows; ++i) {
     const unsigned t = t0 + i * R::kRows;
     sk[i] = sv[i] = 0.f;
 #pragma unroll
@@ -241,7 +242,7 @@ __global__ void __launch_bounds__(kPoolThreads) pool_read_kernel(const char* __r
     }
   }
 #pragma unroll
-  for (int i = 0; i < kRowsPerThread; ++i) {
+  for (int i = 0; i < kReadRows; ++i) {
     const unsigned t = t0 + i * R::kRows;
     if (t >= n) continue;
     uint4* ko = reinterpret_cast<uint4*>(k + t * ts + at);
@@ -249,8 +250,8 @@ __global__ void __launch_bounds__(kPoolThreads) pool_read_kernel(const char* __r
 #pragma unroll
     for (int j = 0; j < 2; ++j) {
       if constexpr (I8) {
-        ko[j * R::kLanes] = from_codes<T>(kr[i][j], sk[i]);
-        vo[j * R::kLanes] = from_codes<T>(vr[i][j], sv[i]);
+        __stcs(ko + j * R::kLanes, from_codes<T>(kr[i][j], sk[i]));
+        __stcs(vo + j * R::kLanes, from_codes<T>(vr[i][j], sv[i]));
       } else {
         ko[j * R::kLanes] = make_uint4(kr[i][j][0], kr[i][j][1], kr[i][j][2], kr[i][j][3]);
         vo[j * R::kLanes] = make_uint4(vr[i][j][0], vr[i][j][1], vr[i][j][2], vr[i][j][3]);

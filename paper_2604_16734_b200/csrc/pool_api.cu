@@ -15,8 +15,8 @@
 
 #include "geom.cuh"
 #include "kernels_cc.cuh"
-#include "kernels_tc.cuh"
 #include "pool.cuh"
+#include "prompt.cuh"
 
 typedef CUresult (*EncodeTiledFn)(CUtensorMap*, CUtensorMapDataType, cuuint32_t, void*, const cuuint64_t*,
                                   const cuuint64_t*, const cuuint32_t*, const cuuint32_t*, CUtensorMapInterleave,
@@ -182,7 +182,7 @@ extern "C" int kvc_pool_write(kvc_pool* c, const void* k, const void* v, long lo
   const kvc_pool_config& cf = c->cfg;
   const cudaError_t e = by_shape(c, [&](auto t, auto d, auto i8) {
     using T = decltype(t);
-    constexpr int D = decltype(d)::value, per = kvc::RowShape<T, D>::kRowTokens;
+    constexpr int D = decltype(d)::value, per = kvc::RowShape<T, D>::kRows * kvc::kWriteRows;
     kvc::pool_write_kernel<T, D, decltype(i8)::value><<<(unsigned)((n + per - 1) / per) * cf.n_kv_heads, kvc::kPoolThreads, 0, (cudaStream_t)stream>>>(
         (const T*)k, (const T*)v, token_stride, head_stride, slots, (unsigned)n, (char*)blob, (char*)workspace, c->geom);
     return cudaGetLastError();
@@ -199,7 +199,7 @@ extern "C" int kvc_pool_read(kvc_pool* c, const void* blob, const long long* slo
   const kvc_pool_config& cf = c->cfg;
   const cudaError_t e = by_shape(c, [&](auto t, auto d, auto i8) {
     using T = decltype(t);
-    constexpr int D = decltype(d)::value, per = kvc::RowShape<T, D>::kRowTokens;
+    constexpr int D = decltype(d)::value, per = kvc::RowShape<T, D>::kRows * kvc::kReadRows;
     kvc::pool_read_kernel<T, D, decltype(i8)::value><<<(unsigned)((n + per - 1) / per) * cf.n_kv_heads, kvc::kPoolThreads, 0, (cudaStream_t)stream>>>(
         (const char*)blob, slots, (unsigned)n, (T*)k, (T*)v, token_stride, head_stride, (char*)workspace, c->geom);
     return cudaGetLastError();
@@ -255,34 +255,28 @@ extern "C" int kvc_pool_decode(kvc_pool* c, const void* q, long long q_stride, c
 }
 
 // ------------------------------------------------------------------------------------------------ prompts
-// Pieces of work: {first token of the prompt, tokens of the prompt, first row tile, row tiles}, longest first.  A row tile is
-// 128 / G tokens on the tensor cores (bf16), BM rows of (token, head) on the CUDA cores (fp32).
-struct PromptItem { int first, len, tile, tiles; };
+// Pieces of work, longest first.  A row tile is 128 / G tokens on the tensor cores (bf16), two to a piece; kPromptRowsCc rows of
+// (token, head) on the CUDA cores (fp32).
+using kvc::PromptItem;
 
 static const int kPromptRowsCc = 32;
-
-static int plan_row_tiles(const kvc_pool* c, long long tiles) {
-  if (c->cfg.dtype == KVC_F32) return kPromptRowsCc;
-  return tiles * c->cfg.n_kv_heads > 2 * kvc::kNumSMs ? 2 : 1;
-}
 
 extern "C" int kvc_pool_plan(kvc_pool* c, const int* lens, int n_seqs, kvc_prompt_plan* plan, void* items) {
   if (!live(c)) return KVC_ESTATE;
   if (!plan || n_seqs < 0 || (n_seqs > 0 && !lens)) return fail(c, KVC_EINVAL, "null pointer argument or n_seqs = %d", n_seqs);
   const bool f32 = c->cfg.dtype == KVC_F32;
   const int G = c->geom.G, TOK = f32 ? 0 : 128 / G;
-  long long tokens = 0, tiles = 0;
+  long long tokens = 0;
   for (int i = 0; i < n_seqs; ++i) {
     if (lens[i] < 0) return fail(c, KVC_EINVAL, "lens[%d] = %d", i, lens[i]);
     tokens += lens[i];
-    tiles += f32 ? ((long long)lens[i] * G + kPromptRowsCc - 1) / kPromptRowsCc : (lens[i] + TOK - 1) / TOK;
   }
   if (tokens * c->cfg.n_q_heads > 0x7fffffffll) return fail(c, KVC_EINVAL, "%lld tokens of %d query heads: 2^31 rows or more", tokens, c->cfg.n_q_heads);
-  const int R = plan_row_tiles(c, tiles);
+  const int R = f32 ? kPromptRowsCc : 2;
   long long n_items = 0;
   for (int i = 0; i < n_seqs; ++i) {
     const long long t = f32 ? ((long long)lens[i] * G + R - 1) / R : (lens[i] + TOK - 1) / TOK;
-    n_items += f32 || R == 1 ? t : (t + 1) / 2;
+    n_items += f32 ? t : (t + 1) / 2;
   }
   if (n_items > 0x7fffffffll) return fail(c, KVC_EINVAL, "%lld pieces of work", n_items);
   plan->n_seqs = n_seqs;
@@ -319,14 +313,19 @@ static int make_map(kvc_pool* c, CUtensorMap* m, const void* base, int d, int he
   return KVC_OK;
 }
 
-template <int D, int R>
-static cudaError_t launch_prompt_tc(const kvc_pool* c, const CUtensorMap (&m)[4], const kvc_prompt_plan* plan, const void* items,
-                                    void* ws, void* out, const kvc::Geom& g, cudaStream_t st) {
-  const int smem = (R + kvc::attn_stages<R>()) * (D / 64) * kvc::kSubTileBytes + 1024;
+template <int D>
+static cudaError_t launch_prompt_tc(const kvc_pool* c, const CUtensorMap (&m)[3], const kvc_prompt_plan* plan, const void* items,
+                                    void* ws, void* out, float* lse, cudaStream_t st) {
+  constexpr int smem = 6 * (D / 64) * kvc::kSubTileBytes + 1024;
   static bool attr_set[kMaxDevices] = {};
-  if (cudaError_t e = opt_in_smem(kvc::attn_tc_kernel<D, R, true>, smem, attr_set, c->cfg.device)) return e;
-  kvc::attn_tc_kernel<D, R, true><<<dim3(plan->n_items, g.Hkv), kvc::kAttnThreads, smem, st>>>(
-      m[0], m[1], m[2], m[1], m[2], m[3], (char*)const_cast<void*>(items), (__nv_bfloat16*)out, (char*)ws, g, 1, 0);
+  if (cudaError_t e = opt_in_smem(kvc::prompt_kernel<D>, smem, attr_set, c->cfg.device)) return e;
+  kvc::PromptGeom g;
+  g.G = c->geom.G; g.Hq = c->geom.Hq; g.Hkv = c->geom.Hkv; g.n_units = plan->n_items * c->geom.Hkv;
+  g.scale_log2 = c->geom.scale_log2;
+  g.wait_limit_k = kvc::kDefaultWaitLimitK;
+  g.items = (const PromptItem*)items;
+  g.lse = lse;
+  kvc::prompt_kernel<D><<<std::min(g.n_units, kvc::kNumSMs), kvc::kAttnThreads, smem, st>>>(m[0], m[1], m[2], (__nv_bfloat16*)out, (char*)ws, g);
   return cudaGetLastError();
 }
 
@@ -347,8 +346,8 @@ extern "C" int kvc_pool_prompt(kvc_pool* c, const void* q, long long q_stride, c
   const kvc_pool_config& cf = c->cfg;
   if (!plan || !workspace) return fail(c, KVC_EINVAL, "null pointer argument");
   const bool f32 = cf.dtype == KVC_F32;
-  if (plan->n_tokens < 0 || plan->n_items < 0 || plan->n_tokens * cf.n_q_heads > 0x7fffffffll || plan->item_bytes != sizeof(PromptItem) * (size_t)plan->n_items ||
-      (f32 ? plan->row_tiles != kPromptRowsCc : plan->row_tiles != 1 && plan->row_tiles != 2))
+  if (plan->n_tokens < 0 || plan->n_items < 0 || (long long)plan->n_items * cf.n_kv_heads > 0x7fffffffll || plan->n_tokens * cf.n_q_heads > 0x7fffffffll || plan->item_bytes != sizeof(PromptItem) * (size_t)plan->n_items ||
+      plan->row_tiles != (f32 ? kPromptRowsCc : 2))
     return fail(c, KVC_EINVAL, "the plan is not one of this pool's");
   if (plan->n_tokens > 0 && (!q || !k || !v || !items || !out)) return fail(c, KVC_EINVAL, "null pointer argument");
   if (!aligned16(q) || !aligned16(k) || !aligned16(v) || !aligned16(items) || !aligned16(workspace) || !aligned16(out) || (reinterpret_cast<uintptr_t>(lse) & 3))
@@ -357,15 +356,15 @@ extern "C" int kvc_pool_prompt(kvc_pool* c, const void* q, long long q_stride, c
     return fail(c, KVC_EINVAL, "strides %lld, %lld: multiples of 16 bytes, at least a token's heads", q_stride, kv_stride);
   if (int rc = check_device(c)) return rc;
   if (plan->n_tokens == 0) return KVC_OK;
-  kvc::Geom g;
-  memset(&g, 0, sizeof(g));
-  g.G = c->geom.G; g.Hq = cf.n_q_heads; g.Hkv = cf.n_kv_heads; g.d = cf.head_dim; g.nl = 1;
-  g.scale_log2 = c->geom.scale_log2;
-  g.q_ls = q_stride; g.kv_ls = kv_stride;
-  g.score_off = (long long)reinterpret_cast<intptr_t>(lse);
-  g.wait_limit_k = kvc::kDefaultWaitLimitK;
   cudaError_t e;
   if (f32) {
+    kvc::Geom g;
+    memset(&g, 0, sizeof(g));
+    g.G = c->geom.G; g.Hq = cf.n_q_heads; g.Hkv = cf.n_kv_heads; g.d = cf.head_dim; g.nl = 1;
+    g.scale_log2 = c->geom.scale_log2;
+    g.q_ls = q_stride; g.kv_ls = kv_stride;
+    g.score_off = (long long)reinterpret_cast<intptr_t>(lse);
+    g.wait_limit_k = kvc::kDefaultWaitLimitK;
     e = cf.head_dim == 128 ? launch_prompt_cc<128>(c, q, k, v, plan, items, workspace, out, g, (cudaStream_t)stream)
                            : launch_prompt_cc<64>(c, q, k, v, plan, items, workspace, out, g, (cudaStream_t)stream);
   } else {
@@ -377,15 +376,13 @@ extern "C" int kvc_pool_prompt(kvc_pool* c, const void* q, long long q_stride, c
         return fail(c, KVC_ECUDA, "cuTensorMapEncodeTiled entry point unavailable: %s", cudaGetErrorString(e));
       c->encode = (EncodeTiledFn)fn;
     }
-    CUtensorMap m[4];
-    const int d = cf.head_dim, TOK = 128 / g.G;
-    if (int rc = make_map(c, &m[0], q, d, g.Hq, plan->n_tokens, q_stride, g.G, TOK)) return rc;
-    if (int rc = make_map(c, &m[1], k, d, g.Hkv, plan->n_tokens, kv_stride, 1, 128)) return rc;
-    if (int rc = make_map(c, &m[2], v, d, g.Hkv, plan->n_tokens, kv_stride, 1, 128)) return rc;
-    if (int rc = make_map(c, &m[3], out, d, g.Hq, plan->n_tokens, (long long)g.Hq * d, g.G, TOK)) return rc;
-    auto run = [&](auto launcher) { return launcher(c, m, plan, items, workspace, out, g, (cudaStream_t)stream); };
-    if (d == 128) e = plan->row_tiles == 2 ? run(launch_prompt_tc<128, 2>) : run(launch_prompt_tc<128, 1>);
-    else e = plan->row_tiles == 2 ? run(launch_prompt_tc<64, 2>) : run(launch_prompt_tc<64, 1>);
+    CUtensorMap m[3];
+    const int d = cf.head_dim, G = c->geom.G;
+    if (int rc = make_map(c, &m[0], q, d, cf.n_q_heads, plan->n_tokens, q_stride, G, 128 / G)) return rc;
+    if (int rc = make_map(c, &m[1], k, d, cf.n_kv_heads, plan->n_tokens, kv_stride, 1, 128)) return rc;
+    if (int rc = make_map(c, &m[2], v, d, cf.n_kv_heads, plan->n_tokens, kv_stride, 1, 128)) return rc;
+    e = d == 128 ? launch_prompt_tc<128>(c, m, plan, items, workspace, out, lse, (cudaStream_t)stream)
+                 : launch_prompt_tc<64>(c, m, plan, items, workspace, out, lse, (cudaStream_t)stream);
   }
   c->launches++;
   return check_cuda(c, e, "prompt launch");

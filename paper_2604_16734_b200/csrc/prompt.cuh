@@ -1,0 +1,422 @@
+// Causal attention of whole prompts of different lengths, packed one after the other (bf16, tensor cores).
+#pragma once
+#include <cuda.h>
+#include "kernels_tc.cuh"
+#include "ptx.cuh"
+
+namespace kvc {
+
+// A piece of work: two row tiles of a prompt for every kv-head.  A row tile is TOK = 128 / G tokens with the G query heads of a
+// kv-head beside each other (row = token * G + head), so keys and values are read once per kv-head.
+struct PromptItem { int first, len, tile, tiles; };        // first token and tokens of the prompt, first row tile, row tiles (1 or 2)
+
+struct PromptGeom {
+  int G, Hq, Hkv, n_units;     // units: (piece, kv-head), kv-heads innermost, most key tiles first
+  float scale_log2;
+  int wait_limit_k;
+  const PromptItem* items;
+  float* lse;                  // [tokens][Hq] or null
+};
+
+// The arithmetic of a key tile is the block attention's with two row tiles (attn_tc_kernel: S = Q K^T and O += P V with tcgen05.mma,
+// accumulators in TMEM, a thread per row, exponentials in turns, lazy rescaling, S ahead of the softmax).  What differs is that a CTA
+// stays: it walks through units c, 2C - 1 - c, 2C + c, ... of C CTAs (there and back, since units are sorted by length), and its ring,
+// barriers and TMEM stay with it.  While the softmax warps write a unit's rows, the next unit's Q, keys and values are already on
+// their way and its first S is computed, so a unit costs its key tiles and about a microsecond.  With a CTA per unit (set-up, TMEM,
+// first loads and the last stores in nobody's shadow) it cost up to ten: 64 prompts of 128 tokens, 32 / 8 heads, d = 128 69 us.
+//   warps 0-3, 4-7  softmax of row tile A, B (216 registers); they write their rows straight from registers: Q's shared memory is
+//                   the next unit's by then
+//   warp  8         TMA producer: Q, then K one tile ahead of V through a ring, two slots each
+//   warp  9, 10     issue S_t = Q_t K_j^T, O_t += P_t V_j
+//   warp  11        zeroes the values behind a prompt's end in its last key tile: the next prompt's rows (or nothing) were loaded there,
+//                   and an infinity or a NaN must not meet a zero probability.  (Its keys are masked like those of later tokens.)
+// TMEM columns: S [0,128)  P_A [128,192)  P_B [192,256)  O_A [256,384)  O_B [384,512).
+// Bound: the key loop, tensor and exponential pipes in turns (one prompt of 16384 tokens: 80 % of a library product's rate).
+// grid min(148, units), block 384, dynamic smem 6 * (D/64) * 16 KB + 1 KB.
+struct SmemPrompt {
+  uint64_t q_full, q_empty, kv_full[4], kv_empty[4], s_full[2], s_free, p_half[2][2], pv_done[2], v_tail, mma_done[2];
+  uint32_t tmem_base;
+  int s_issued;
+  int wait_ctl[2];
+};
+
+template <int D>
+__global__ void __launch_bounds__(kAttnThreads, 1) prompt_kernel(const __grid_constant__ CUtensorMap tm_q,
+                                                                  const __grid_constant__ CUtensorMap tm_k,
+                                                                  const __grid_constant__ CUtensorMap tm_v,
+                                                                  __nv_bfloat16* __restrict__ out, char* __restrict__ ws, PromptGeom p) {
+  constexpr int NSUB = D / 64, TILE_BYTES = NSUB * kSubTileBytes, kSlots = 2;
+  constexpr uint32_t TMEM_COLS = 512;
+  constexpr float kRescaleThreshold = 8.f;      // log2 units
+  extern __shared__ uint8_t smem_raw[];
+  uint8_t* smem = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~uintptr_t(1023));
+  uint8_t* sQ = smem;                            // two tiles
+  uint8_t* ring = smem + 2 * TILE_BYTES;         // K, K, V, V
+  __shared__ SmemPrompt sh;
+  const int TOK = 128 / p.G, rows = TOK * p.G;
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  volatile int* abort_flag = sh.wait_ctl;
+
+  // the k-th unit of this CTA (-1: none), its piece, its key tiles
+  auto unit_of = [&](int k) {
+    const int u = k * gridDim.x + (k & 1 ? gridDim.x - 1 - blockIdx.x : blockIdx.x);
+    return u < p.n_units ? u : -1;
+  };
+  auto piece_of = [&](int u) { return u < 0 ? make_int4(0, 0, 0, 0) : *reinterpret_cast<const int4*>(p.items + u / p.Hkv); };
+  auto tiles_of = [&](const int4& it) { return (min((it.z + 2) * TOK, it.y) + 127) / 128; };
+
+  if (threadIdx.x == 0) {
+    mbar_init(&sh.q_full, 2); mbar_init(&sh.q_empty, 1); mbar_init(&sh.s_free, 4); mbar_init(&sh.v_tail, 1);
+    for (int i = 0; i < 2; ++i) {
+      mbar_init(&sh.s_full[i], 1); mbar_init(&sh.pv_done[i], 1); mbar_init(&sh.mma_done[i], 1);
+      mbar_init(&sh.p_half[i][0], 4); mbar_init(&sh.p_half[i][1], 4);     // one arrival per softmax warp
+    }
+    for (int i = 0; i < 4; ++i) { mbar_init(&sh.kv_full[i], 1); mbar_init(&sh.kv_empty[i], 1); }
+    sh.s_issued = -1;
+    sh.wait_ctl[0] = 0; sh.wait_ctl[1] = p.wait_limit_k;
+    mbar_fence_init();
+  }
+  {                                              // rows of the Q tiles that TMA never writes must be finite
+    const int pad16 = (128 - rows) * 8;          // 16-byte units per sub-tile
+    for (int i = threadIdx.x; i < 2 * NSUB * pad16; i += blockDim.x)
+      reinterpret_cast<uint4*>(sQ + i / pad16 * kSubTileBytes + rows * 128)[i % pad16] = make_uint4(0, 0, 0, 0);
+  }
+  fence_proxy_async_smem();
+  if (warp == 8) {
+    tmem_alloc(&sh.tmem_base, TMEM_COLS);
+    tmem_relinquish();
+  }
+  tc_fence_before_sync();
+  __syncthreads();
+  tc_fence_after_sync();
+  const uint32_t tmem = sh.tmem_base;
+
+  if (warp >= 8) {
+    reg_dec<56>();
+    if (warp == 8) {
+      // ---------------------------------------------------------------- TMA producer
+      if (lane == 0) {
+        tma_prefetch_desc(&tm_q); tma_prefetch_desc(&tm_k); tma_prefetch_desc(&tm_v);
+        uint32_t q_loads = 0, loads[4] = {0, 0, 0, 0};         // how many loads a barrier has been armed for
+        bool ok = true;
+        auto load_tile = [&](int n, int v, int tok, int g) {   // K (v = 0) or V (1) of the n-th key tile of this CTA
+          const int slot = v * kSlots + n % kSlots, round = n / kSlots;
+          ok = ok && (round == 0 || mbar_wait(&sh.kv_empty[slot], (round - 1) & 1, abort_flag));
+          if (!ok) return;
+          mbar_expect_tx(&sh.kv_full[slot], TILE_BYTES);
+          loads[slot] = round + 1;
+          for (int sub = 0; sub < NSUB; ++sub)                 // (tokens past the last prompt are zero-filled)
+            tma_load_4d(ring + slot * TILE_BYTES + sub * kSubTileBytes, v ? &tm_v : &tm_k, &sh.kv_full[slot], sub * 64, g, tok, 0);
+        };
+        auto load_q = [&](int k, const int4& it, int g) {
+          ok = ok && (k == 0 || mbar_wait(&sh.q_empty, (k - 1) & 1, abort_flag));
+          if (!ok) return;
+          q_loads = k + 1;
+          for (int t = 0; t < 2; ++t) {
+            mbar_expect_tx(&sh.q_full, NSUB * rows * 128);
+            for (int sub = 0; sub < NSUB; ++sub)
+              tma_load_4d(sQ + t * TILE_BYTES + sub * kSubTileBytes, &tm_q, &sh.q_full, sub * 64, g * p.G, it.x + (it.z + t) * TOK, 0);
+          }
+        };
+        int n = 0, v_tok = 0, v_g = 0;                         // key tiles so far; where the V tile that is still to come stands
+        int u = unit_of(0);
+        int4 it = piece_of(u);
+        for (int k = 0; u >= 0 && ok; ++k) {
+          const int u_next = unit_of(k + 1);
+          const int4 next = piece_of(u_next);
+          const int g = u % p.Hkv, T = tiles_of(it);
+          if (k == 0) load_q(0, it, g);
+          for (int j = 0; j < T && ok; ++j, ++n) {
+            load_tile(n, 0, it.x + j * 128, g);
+            if (n > 0) load_tile(n - 1, 1, v_tok, v_g);
+            if (j == 0 && k > 0) load_q(k, it, g);             // (behind the last V of the unit before: that is wanted first)
+            v_tok = it.x + j * 128; v_g = g;
+          }
+          u = u_next;
+          it = next;
+        }
+        if (n > 0 && ok) load_tile(n - 1, 1, v_tok, v_g);
+        // The block keeps its shared memory until all loads have landed, whoever has given up waiting for them.
+        if (q_loads) mbar_drain(&sh.q_full, (q_loads - 1) & 1);
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+          if (loads[i]) mbar_drain(&sh.kv_full[i], (loads[i] - 1) & 1);
+      }
+    } else if (warp == 9) {
+      // ---------------------------------------------------------------- issuer of S = Q K^T
+      if (lane == 0) {
+        constexpr uint32_t idesc_qk = idesc_bf16_f32(128, 128, 0, 0);
+        constexpr uint32_t hi = smem_desc_hi_sw128(1024);
+        const uint32_t q_lo0 = smem_desc_lo(smem_u32(sQ), 16), k_lo0 = smem_desc_lo(smem_u32(ring), 16);   // K-major operands
+        bool ok = true;
+        int n = 0, s = 0;                                      // key tiles and S so far
+        int u = unit_of(0);
+        int4 it = piece_of(u);
+        for (int k = 0; u >= 0 && ok; ++k) {
+          const int u_next = unit_of(k + 1);
+          const int4 next = piece_of(u_next);
+          const int T = tiles_of(it);
+          ok = mbar_wait(&sh.q_full, k & 1, abort_flag);
+          for (int i = 0; i < 2 * T && ok; ++i, ++s) {
+            const int t = i & 1, slot = n % kSlots;
+            if (t == 0) ok = mbar_wait(&sh.kv_full[slot], (n / kSlots) & 1, abort_flag);
+            if (ok && s > 0) ok = mbar_wait_spin(&sh.s_free, (s - 1) & 1, abort_flag);
+            if (!ok) break;
+            tc_fence_after_sync();
+            const uint32_t q_lo = q_lo0 + t * (TILE_BYTES >> 4), k_lo = k_lo0 + slot * (TILE_BYTES >> 4);
+#pragma unroll
+            for (int kk = 0; kk < D / 16; ++kk) {
+              const uint32_t off = ((kk / 4) * kSubTileBytes + (kk % 4) * 32) >> 4;
+              mma_ss_lh(tmem, q_lo + off, hi, k_lo + off, hi, idesc_qk, kk > 0);
+            }
+            mma_commit(&sh.s_full[t]);
+            *static_cast<volatile int*>(&sh.s_issued) = s;
+            if (t == 1) { mma_commit(&sh.kv_empty[slot]); ++n; }
+          }
+          if (ok) mma_commit(&sh.q_empty);
+          u = u_next;
+          it = next;
+        }
+      }
+    } else if (warp == 10) {
+      // ---------------------------------------------------------------- issuer of O_t += P_t V_j, half by half
+      if (lane == 0) {
+        constexpr uint32_t idesc_pv = idesc_bf16_f32(128, D, 0, 1);
+        constexpr uint32_t hi = smem_desc_hi_sw128(1024);
+        const uint32_t v_lo0 = smem_desc_lo(smem_u32(ring) + kSlots * TILE_BYTES, kSubTileBytes);   // MN-major operand
+        bool ok = true;
+        int n = 0, s = 0;                                      // key tiles and S so far (of the units before: s)
+        int u = unit_of(0);
+        int4 it = piece_of(u);
+        for (int k = 0; u >= 0 && ok; ++k) {
+          const int u_next = unit_of(k + 1);
+          const int4 next = piece_of(u_next);
+          const int T = tiles_of(it);
+          const bool tail = T * 128 > it.y;
+          for (int i = 0; i < 2 * T && ok; ++i) {
+            const int t = i & 1, j = i >> 1, slot = n % kSlots;
+            if (t == 0) {
+              ok = mbar_wait(&sh.kv_full[kSlots + slot], (n / kSlots) & 1, abort_flag);
+              // (v_tail, first phase: the tile before the last one in its slot has been seen, so that warp 11 may wait for the last
+              // by its parity; second phase: the last one is as it should be)
+              if (tail && ok && j == max(T - 1 - kSlots, 0)) mbar_arrive(&sh.v_tail);
+              if (tail && j == T - 1) ok = ok && mbar_wait(&sh.v_tail, 1, abort_flag);
+            }
+            const uint32_t v_lo = v_lo0 + slot * (TILE_BYTES >> 4), tP = tmem + 128 + t * 64, tO = tmem + 256 + t * 128;
+#pragma unroll
+            for (int half = 0; half < 2; ++half) {
+              ok = ok && mbar_wait_spin(&sh.p_half[t][half], n & 1, abort_flag);
+              // the S of the item after next goes first: that one is wanted soon
+              if (half == 0) ok = ok && word_wait_spin(&sh.s_issued, s + min(i + 2, 2 * T - 1), abort_flag);
+              if (!ok) break;
+              tc_fence_after_sync();
+#pragma unroll
+              for (int kk = 4 * half; kk < 4 * half + 4; ++kk)   // 16 keys per MMA
+                mma_ts_lh(tO, tP + kk * 8, v_lo + kk * (2048 >> 4), hi, idesc_pv, j > 0 || kk > 0);
+            }
+            if (!ok) break;
+            mma_commit(&sh.pv_done[t]);
+            if (t == 1) { mma_commit(&sh.kv_empty[kSlots + slot]); ++n; }
+          }
+          s += 2 * T;
+          u = u_next;
+          it = next;
+        }
+      }
+    } else {
+      // ---------------------------------------------------------------- values behind a prompt's end
+      int n = 0;                                               // key tiles so far
+      bool ok = true;
+      int u = unit_of(0);
+      int4 it = piece_of(u);
+      for (int k = 0; u >= 0 && ok; ++k) {
+        const int u_next = unit_of(k + 1);
+        const int4 next = piece_of(u_next);
+        const int T = tiles_of(it);
+        n += T;
+        if (T * 128 > it.y) {
+          const int slot = kSlots + (n - 1) % kSlots, seen = it.y - (T - 1) * 128;
+          ok = mbar_wait(&sh.v_tail, 0, abort_flag);
+          ok = __all_sync(0xffffffffu, ok && mbar_wait(&sh.kv_full[slot], ((n - 1) / kSlots) & 1, abort_flag));
+          if (ok) {
+            for (int sub = 0; sub < NSUB; ++sub)
+              for (int i = seen * 8 + lane; i < 128 * 8; i += 32)
+                reinterpret_cast<uint4*>(ring + slot * TILE_BYTES + sub * kSubTileBytes)[i] = make_uint4(0, 0, 0, 0);
+            fence_proxy_async_smem();
+            __syncwarp();
+            if (lane == 0) mbar_arrive(&sh.v_tail);
+          }
+        }
+        u = u_next;
+        it = next;
+      }
+    }
+    __syncwarp();
+    // TMEM is given back when the softmax warps have read it for the last time and, after a wait that ran out, the issuers' MMAs are
+    // complete (as in attn_tc_kernel).
+    if (warp == 9 || warp == 10) {
+      named_barrier(6, 256 + 64);
+      if (__builtin_expect(abort_flag[0] != 0, 0) && lane == 0) {
+        mma_commit(&sh.mma_done[warp - 9]);
+        mbar_drain(&sh.mma_done[warp - 9], 0);
+      }
+      __syncwarp();
+      named_barrier_arrive(7, 96);
+    }
+    if (warp == 8) {
+      named_barrier(7, 96);
+      tc_fence_after_sync();
+      tmem_dealloc(tmem, TMEM_COLS);
+    }
+  } else {
+    reg_inc<216>();
+    // ---------------------------------------------------------------- softmax and rows of tile t
+    const int t = warp >> 2;
+    const int r = (warp & 3) * 32 + lane;                     // row of the tile = TMEM lane
+    const int r_tok = r / p.G, hh = r % p.G;
+    const uint32_t lane_addr = static_cast<uint32_t>((warp & 3) * 32) << 16;
+    const uint32_t tmem_S = tmem + lane_addr, tmem_P = tmem + 128 + t * 64 + lane_addr, tmem_O = tmem + 256 + t * 128 + lane_addr;
+    bool ok = true;
+    int n = 0;                                                 // key tiles so far
+    int u = unit_of(0);
+    int4 it = piece_of(u);
+    for (int k = 0; u >= 0; ++k) {
+      const int T = tiles_of(it);
+      const int tok0 = (it.z + t) * TOK, tok = tok0 + r_tok;
+      float m_ref = -INFINITY, l = 0.f;                        // reference maximum (log2 units) and row sum
+      if (t == 1 && k == 0) named_barrier_arrive(2, 256);      // the turns (named barrier 2 + t: "group t may go") start with group 0
+      for (int j = 0; j < T; ++j, ++n) {
+        // Waits that gave up only skip the arithmetic: the turn barrier is passed on every path, once per key tile and warp.
+        if (ok) ok = __all_sync(0xffffffffu, mbar_wait(&sh.s_full[t], n & 1, abort_flag));
+        bool took_turn = false, told = false;
+        const bool hand_over = t == 0 || j + 1 < T || unit_of(k + 1) >= 0;   // the other group has a key tile left, here or in the next unit
+        if (ok) do {
+          tc_fence_after_sync();
+          uint32_t sr[128];
+#pragma unroll
+          for (int c = 0; c < 4; ++c) tmem_ld32(tmem_S + c * 32, sr + c * 32);
+          const bool pv_ready = j > 0 && mbar_test_wait(&sh.pv_done[t], (n - 1) & 1);
+          tmem_wait_ld();
+          tc_fence_before_sync();
+          __syncwarp();
+          if (lane == 0) mbar_arrive(&sh.s_free);              // the other group's next S may be computed
+          // columns [0, lim) of this tile are visible: up to the row's own token
+          if (__builtin_expect((j + 1) * 128 > tok0 + 1, 0)) {
+            const int lim = tok + 1 - j * 128;
+#pragma unroll
+            for (int c = 0; c < 128; ++c)
+              if (c >= lim) sr[c] = 0xff800000u;               // -inf
+          }
+          float mx4[8];
+#pragma unroll
+          for (int i = 0; i < 8; ++i) mx4[i] = fmaxf(__uint_as_float(sr[i]), __uint_as_float(sr[8 + i]));
+#pragma unroll
+          for (int c = 16; c < 128; c += 16) {
+#pragma unroll
+            for (int i = 0; i < 8; ++i) mx4[i] = fmax3(mx4[i], __uint_as_float(sr[c + i]), __uint_as_float(sr[c + 8 + i]));
+          }
+          const float mx = fmaxf(fmax3(mx4[0], mx4[1], mx4[2]), fmaxf(fmax3(mx4[3], mx4[4], mx4[5]), fmaxf(mx4[6], mx4[7])));
+          const float m_new = mx * p.scale_log2;               // scale > 0
+          const bool grow = m_new > m_ref + kRescaleThreshold; // (first tile: m_ref is -infinity)
+          if (__builtin_expect(__any_sync(0xffffffffu, grow || !pv_ready), 0)) {
+            if (j == 0) {
+              m_ref = m_new == -INFINITY ? 0.f : m_new;
+            } else {
+              ok = __all_sync(0xffffffffu, mbar_wait(&sh.pv_done[t], (n - 1) & 1, abort_flag));
+              if (!ok) break;
+              if (__any_sync(0xffffffffu, grow)) {
+                tc_fence_after_sync();
+                const float f = grow ? fast_exp2(m_ref - m_new) : 1.f;
+                if (grow) { m_ref = m_new; l *= f; }
+#pragma unroll
+                for (int c = 0; c < D / 32; ++c) {
+                  uint32_t o[32];
+                  tmem_ld32(tmem_O + c * 32, o);
+                  tmem_wait_ld();
+#pragma unroll
+                  for (int i = 0; i < 32; ++i) o[i] = __float_as_uint(__uint_as_float(o[i]) * f);
+                  tmem_st32(tmem_O + c * 32, o);
+                }
+              }
+            }
+          }
+          tc_fence_after_sync();
+          named_barrier(2 + t, 256);
+          took_turn = true;
+          const uint64_t scale2 = f32x2(p.scale_log2, p.scale_log2), neg_m2 = f32x2(-m_ref, -m_ref);
+          uint64_t ps2[2] = {f32x2(0.f, 0.f), f32x2(0.f, 0.f)};
+#pragma unroll
+          for (int c = 0; c < 4; ++c) {
+            uint32_t pk[16];
+#pragma unroll
+            for (int i = 0; i < 16; ++i) {
+              float x0, x1;
+              f32x2_split(fma_f32x2(f32x2(__uint_as_float(sr[c * 32 + 2 * i]), __uint_as_float(sr[c * 32 + 2 * i + 1])), scale2, neg_m2), x0, x1);
+              const float p0 = fast_exp2(x0), p1 = fast_exp2(x1);
+              ps2[i & 1] = add_f32x2(ps2[i & 1], f32x2(p0, p1));
+              pk[i] = pack_bf16x2(p0, p1);
+            }
+            if (c == 2) {                                      // the first 64 keys of P have landed: the MMA warp may take them
+              tmem_wait_st();
+              tc_fence_before_sync();
+              __syncwarp();
+              if (lane == 0) mbar_arrive(&sh.p_half[t][0]);
+            }
+            tmem_st16(tmem_P + c * 16, pk);
+            if (c == 3) { if (hand_over) named_barrier_arrive(3 - t, 256); told = true; }
+          }
+          {
+            float ps[4];
+            f32x2_split(ps2[0], ps[0], ps[1]);
+            f32x2_split(ps2[1], ps[2], ps[3]);
+            l += (ps[0] + ps[1]) + (ps[2] + ps[3]);
+          }
+          tmem_wait_st();
+          tc_fence_before_sync();
+          __syncwarp();
+          if (lane == 0) mbar_arrive(&sh.p_half[t][1]);
+        } while (0);
+        if (!took_turn) named_barrier(2 + t, 256);             // a wait gave up before the turn was taken: take it now
+        if (!told && hand_over) named_barrier_arrive(3 - t, 256);
+      }
+      // ---- the unit's rows
+      const int u_next = unit_of(k + 1);
+      const int4 next = piece_of(u_next);
+      ok = ok && mbar_wait(&sh.pv_done[t], (n - 1) & 1, abort_flag);
+      ok = __all_sync(0xffffffffu, ok);                        // the TMEM accesses below are warp-wide
+      if (ok) {
+        tc_fence_after_sync();
+        const bool row_valid = r < rows && tok < it.y;
+        const long long row = static_cast<long long>(it.x + tok) * p.Hq + u % p.Hkv * p.G + hh;
+        const float inv = 1.f / l;
+        __nv_bfloat16* dst = out + row * D;
+#pragma unroll
+        for (int c = 0; c < D / 32; ++c) {
+          uint32_t o[32], pk[16];
+          tmem_ld32(tmem_O + c * 32, o);
+          tmem_wait_ld();
+#pragma unroll
+          for (int i = 0; i < 16; ++i) pk[i] = pack_bf16x2(__uint_as_float(o[2 * i]) * inv, __uint_as_float(o[2 * i + 1]) * inv);
+          if (row_valid) {
+            if ((reinterpret_cast<uintptr_t>(out) & 31) == 0) {
+              st_global_v8(dst + c * 32, pk);
+              st_global_v8(dst + c * 32 + 16, pk + 8);
+            } else {
+#pragma unroll
+              for (int i = 0; i < 4; ++i) reinterpret_cast<uint4*>(dst + c * 32)[i] = make_uint4(pk[4 * i], pk[4 * i + 1], pk[4 * i + 2], pk[4 * i + 3]);
+            }
+          }
+        }
+        if (row_valid && p.lse) p.lse[row] = (m_ref + log2f(l)) * 0.6931471805599453f;
+        tc_fence_before_sync();                                // O is read: the next unit's P, behind which its first P V comes
+      }
+      u = u_next;
+      it = next;
+    }
+    tc_fence_before_sync();
+    named_barrier_arrive(6, 256 + 64);
+  }
+  if (lane == 0 && abort_flag[0]) atomicExch(reinterpret_cast<int*>(ws), -4 /* KVC_ETIMEOUT */);   // (a warp's own waits are over)
+}
+
+}  // namespace kvc
