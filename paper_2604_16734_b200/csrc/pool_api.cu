@@ -316,7 +316,7 @@ static int make_map(kvc_pool* c, CUtensorMap* m, const void* base, int d, int he
 template <int D>
 static cudaError_t launch_prompt_tc(const kvc_pool* c, const CUtensorMap (&m)[3], const kvc_prompt_plan* plan, const void* items,
                                     void* ws, void* out, float* lse, cudaStream_t st) {
-  constexpr int smem = 6 * (D / 64) * kvc::kSubTileBytes + 1024;
+  constexpr int smem = (6 * (D / 64) + 2) * kvc::kSubTileBytes + 1024;
   static bool attr_set[kMaxDevices] = {};
   if (cudaError_t e = opt_in_smem(kvc::prompt_kernel<D>, smem, attr_set, c->cfg.device)) return e;
   kvc::PromptGeom g;

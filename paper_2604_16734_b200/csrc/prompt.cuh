@@ -24,15 +24,16 @@ struct PromptGeom {
 // barriers and TMEM stay with it.  While the softmax warps write a unit's rows, the next unit's Q, keys and values are already on
 // their way and its first S is computed, so a unit costs its key tiles and about a microsecond.  With a CTA per unit (set-up, TMEM,
 // first loads and the last stores in nobody's shadow) it cost up to ten: 64 prompts of 128 tokens, 32 / 8 heads, d = 128 69 us.
-//   warps 0-3, 4-7  softmax of row tile A, B (216 registers); they write their rows straight from registers: Q's shared memory is
-//                   the next unit's by then
+//   warps 0-3, 4-7  softmax of row tile A, B (216 registers); a warp's rows leave through a stage of its own, 64 columns at a time, as
+//                   whole lines (Q's shared memory is the next unit's by then; 32 bytes of 32 rows per store, straight from
+//                   registers, took 2500 cycles a unit, and so did TMA, whose second half waits for the first to leave)
 //   warp  8         TMA producer: Q, then K one tile ahead of V through a ring, two slots each
 //   warp  9, 10     issue S_t = Q_t K_j^T, O_t += P_t V_j
 //   warp  11        zeroes the values behind a prompt's end in its last key tile: the next prompt's rows (or nothing) were loaded there,
 //                   and an infinity or a NaN must not meet a zero probability.  (Its keys are masked like those of later tokens.)
 // TMEM columns: S [0,128)  P_A [128,192)  P_B [192,256)  O_A [256,384)  O_B [384,512).
 // Bound: the key loop, tensor and exponential pipes in turns (one prompt of 16384 tokens: 80 % of a library product's rate).
-// grid min(148, units), block 384, dynamic smem 6 * (D/64) * 16 KB + 1 KB.
+// grid min(148, units), block 384, dynamic smem 6 * (D/64) * 16 KB + 33 KB.
 struct SmemPrompt {
   uint64_t q_full, q_empty, kv_full[4], kv_empty[4], s_full[2], s_free, p_half[2][2], pv_done[2], v_tail, mma_done[2];
   uint32_t tmem_base;
@@ -52,6 +53,7 @@ __global__ void __launch_bounds__(kAttnThreads, 1) prompt_kernel(const __grid_co
   uint8_t* smem = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~uintptr_t(1023));
   uint8_t* sQ = smem;                            // two tiles
   uint8_t* ring = smem + 2 * TILE_BYTES;         // K, K, V, V
+  uint8_t* stage = ring + 4 * TILE_BYTES;        // per softmax warp: 64 columns of its rows on their way out
   __shared__ SmemPrompt sh;
   const int TOK = 128 / p.G, rows = TOK * p.G;
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
@@ -386,30 +388,37 @@ __global__ void __launch_bounds__(kAttnThreads, 1) prompt_kernel(const __grid_co
       ok = __all_sync(0xffffffffu, ok);                        // the TMEM accesses below are warp-wide
       if (ok) {
         tc_fence_after_sync();
-        const bool row_valid = r < rows && tok < it.y;
-        const long long row = static_cast<long long>(it.x + tok) * p.Hq + u % p.Hkv * p.G + hh;
+        // (fewer than 2^31 rows; -1: the row is none of the prompt's)
+        const int row = r < rows && tok < it.y ? (it.x + tok) * p.Hq + u % p.Hkv * p.G + hh : -1;
         const float inv = 1.f / l;
-        __nv_bfloat16* dst = out + row * D;
+        uint8_t* mine = stage + warp * 4096;
 #pragma unroll
-        for (int c = 0; c < D / 32; ++c) {
-          uint32_t o[32], pk[16];
-          tmem_ld32(tmem_O + c * 32, o);
+        for (int sub = 0; sub < NSUB; ++sub) {
+          uint32_t o[64];
+          tmem_ld32(tmem_O + sub * 64, o);
+          tmem_ld32(tmem_O + sub * 64 + 32, o + 32);
           tmem_wait_ld();
 #pragma unroll
-          for (int i = 0; i < 16; ++i) pk[i] = pack_bf16x2(__uint_as_float(o[2 * i]) * inv, __uint_as_float(o[2 * i + 1]) * inv);
-          if (row_valid) {
-            if ((reinterpret_cast<uintptr_t>(out) & 31) == 0) {
-              st_global_v8(dst + c * 32, pk);
-              st_global_v8(dst + c * 32 + 16, pk + 8);
-            } else {
-#pragma unroll
-              for (int i = 0; i < 4; ++i) reinterpret_cast<uint4*>(dst + c * 32)[i] = make_uint4(pk[4 * i], pk[4 * i + 1], pk[4 * i + 2], pk[4 * i + 3]);
-            }
+          for (int i = 0; i < 8; ++i) {
+            uint4 w;
+            w.x = pack_bf16x2(__uint_as_float(o[8 * i + 0]) * inv, __uint_as_float(o[8 * i + 1]) * inv);
+            w.y = pack_bf16x2(__uint_as_float(o[8 * i + 2]) * inv, __uint_as_float(o[8 * i + 3]) * inv);
+            w.z = pack_bf16x2(__uint_as_float(o[8 * i + 4]) * inv, __uint_as_float(o[8 * i + 5]) * inv);
+            w.w = pack_bf16x2(__uint_as_float(o[8 * i + 6]) * inv, __uint_as_float(o[8 * i + 7]) * inv);
+            *reinterpret_cast<uint4*>(mine + lane * 128 + ((i ^ (lane & 7)) << 4)) = w;
           }
+          __syncwarp();
+#pragma unroll
+          for (int i = 0; i < 8; ++i) {                        // eight lanes to a row: whole lines
+            const int from = i * 4 + (lane >> 3), dst = __shfl_sync(0xffffffffu, row, from);
+            const uint4 w = *reinterpret_cast<const uint4*>(mine + from * 128 + (((lane & 7) ^ (from & 7)) << 4));
+            if (dst >= 0) reinterpret_cast<uint4*>(out + static_cast<long long>(dst) * D + sub * 64)[lane & 7] = w;
+          }
+          __syncwarp();
         }
-        if (row_valid && p.lse) p.lse[row] = (m_ref + log2f(l)) * 0.6931471805599453f;
-        tc_fence_before_sync();                                // O is read: the next unit's P, behind which its first P V comes
+        if (row >= 0 && p.lse) p.lse[row] = (m_ref + log2f(l)) * 0.6931471805599453f;
       }
+      tc_fence_before_sync();                                  // O is read: the next unit's P, behind which its first P V comes
       u = u_next;
       it = next;
     }
