@@ -305,7 +305,7 @@ struct DecodeShape {
   // waits and the way from tile to tile is walked half as often.
   template <int N> static __host__ __device__ constexpr int keys() { return N == 2 || (F32 && D == 128) ? 16 : 32; }
   template <int N> static __host__ __device__ constexpr int stage() { return keys<N>() * (2 * ROWB + (I8 ? 8 : 0)); }   // K, V, scales of both
-  template <int N> static __host__ __device__ constexpr int piece() { return 8 * N * (D + 4) * 4; }
+  template <int N> static __host__ __device__ constexpr int piece() { return 8 * N * (D + 8) * 4; }
   template <int N> static __host__ __device__ constexpr int warps() {
     return F32 && D == 128 ? 5 : N == 2 ? 8 : I8 ? 8 : D == 128 ? 6 : F32 ? 6 : 8;
   }
@@ -316,9 +316,10 @@ struct DecodeShape {
   }
   template <int N> static __host__ __device__ constexpr int warp_bytes() { return (stages<N>() * stage<N>() + OWN + piece<N>() + 127) / 128 * 128; }
 };
-static constexpr int kDecodeMaxCtas = kNumSMs * 2;
-__host__ __device__ constexpr int decode_row(int D) { return D + 4; }    // floats of a head's row of a piece: O, m, l
-static constexpr int kDecodePieceFloats = 16 * (128 + 4);   // a piece in the workspace: up to 16 heads
+static constexpr int kDecodeMaxCtas = kNumSMs;
+// A head's row of a piece: O in D floats, then m, l, and for the join the piece's factor and the joined m and l.
+__host__ __device__ constexpr int decode_row(int D) { return D + 8; }
+static constexpr int kDecodePieceFloats = 16 * (128 + 8);   // a piece in the workspace: up to 16 heads
 
 __device__ __forceinline__ void mma_bf16(float* d, const uint32_t* a, uint32_t b0, uint32_t b1) {
   asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, {%0, %1, %2, %3};"
@@ -743,7 +744,7 @@ struct Decoder {
   }
 };
 
-// Pieces are joined as o = sum_i 2^(m_i - m) o_i, l likewise.  A piece: [heads][decode_row(D)], a row is O, then m and l.
+// Pieces are joined as o = sum_i 2^(m_i - m) o_i, l likewise, m the largest m_i.  A piece: [heads][decode_row(D)].
 template <typename T, int D, bool I8, int NT>
 __global__ void __launch_bounds__(DecodeShape<T, D, I8>::template warps<NT>() * 32, 1) pool_decode_kernel(const T* __restrict__ q, long long q_stride,
                                                                      const T* __restrict__ k_new, const T* __restrict__ v_new,
@@ -756,11 +757,12 @@ __global__ void __launch_bounds__(DecodeShape<T, D, I8>::template warps<NT>() * 
   constexpr int H = 8 * NT, RS = decode_row(D), LANES = D / Piece<T>::N, NS = S::template stages<NT>(), STAGE = S::template stage<NT>(), TK = Dec::TK,
                 WB = S::template warp_bytes<NT>();
   constexpr int kDecodeWarps = S::template warps<NT>(), kDecodeThreads = kDecodeWarps * 32;
+  static_assert(kDecodeWarps * WB >= (kDecodeMaxCtas + 1) * H * 8 + kDecodeThreads * 16, "the last join");
   static_assert(NS >= 2 && NS * STAGE >= S::template piece<NT>(), "two tiles on their way; the last piece overlays the ring");
   extern __shared__ __align__(128) uint8_t smem_b[];          // per warp: ring, own row, first piece; then the line of work
   int* pre = reinterpret_cast<int*>(smem_b + kDecodeWarps * WB);           // [n_seqs + 1] tiles of one head before a sequence
   uint8_t* last = reinterpret_cast<uint8_t*>(pre + n_seqs + 1);            // [n_seqs] rows of a sequence's last tile
-  __shared__ int s_seg[kDecodeWarps][2], s_scan[kDecodeWarps], s_last;
+  __shared__ int s_seg[kDecodeWarps][2], s_scan[kDecodeWarps], s_last[2];
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
   uint8_t* ring = smem_b + warp * WB;
   uint8_t* own_codes = ring + NS * STAGE;
@@ -811,7 +813,7 @@ __global__ void __launch_bounds__(DecodeShape<T, D, I8>::template warps<NT>() * 
     const int sq = sequence_of(x), tiles = pre[sq + 1] - pre[sq], before = (x - pre[sq] * HH) % tiles, behind = tiles - before;
     return min(before, behind) > near ? x : before <= behind ? x - before : x + behind;
   };
-  const int a = boundary(blockIdx.x), e = boundary(blockIdx.x + 1);
+  const int mine = boundary(blockIdx.x + (lane & 1)), a = __shfl_sync(0xffffffffu, mine, 0), e = __shfl_sync(0xffffffffu, mine, 1);
 
   // sequences without a row
   for (int i = blockIdx.x; i < n_seqs; i += gridDim.x)
@@ -998,31 +1000,51 @@ __global__ void __launch_bounds__(DecodeShape<T, D, I8>::template warps<NT>() * 
     store4<T>(out + to * D + d4 * 4, make_float4(o.x * inv, o.y * inv, o.z * inv, o.w * inv));
     if (lse && d4 == 0) lse[to] = l != 0.f ? (m + log2f(l)) * 0.6931471805599453f : -INFINITY;
   };
-  const int* seg_of = &s_seg[0][0];
-  for (int i = 0; i < 2 * kDecodeWarps;) {
-    const int seg = seg_of[i];
-    if (seg < 0) { ++i; continue; }
-    int j = i + 1;                                           // pieces [i, j), some of which may be unused
-    while (j < 2 * kDecodeWarps && (seg_of[j] < 0 || seg_of[j] == seg)) ++j;
+  // Every warp sees the pieces' segments; pieces of one segment are a group.
+  constexpr int P = 2 * kDecodeWarps;
+  static_assert(P <= 32);
+  const int seg_l = lane < P ? (&s_seg[0][0])[lane] : -1;
+  const uint32_t group_l = __match_any_sync(0xffffffffu, seg_l);
+  // factors: a thread per (piece, head)
+  for (int y = threadIdx.x; y < (P * H + 31) / 32 * 32; y += kDecodeThreads) {      // (whole warps, for the shuffles)
+    const int k = min(y / H, P - 1), h = y % H;
+    const uint32_t group = __shfl_sync(0xffffffffu, group_l, k);
+    if (__shfl_sync(0xffffffffu, seg_l, k) < 0 || y >= P * H) continue;
+    float mk[P], m = -INFINITY, l = 0.f;
+#pragma unroll
+    for (int i = 0; i < P; ++i) { mk[i] = group >> i & 1u ? piece_at(i)[h * RS + D] : -INFINITY; m = fmaxf(m, mk[i]); }
+#pragma unroll
+    for (int i = 0; i < P; ++i)
+      if (group >> i & 1u) l = fmaf(mk[i] == -INFINITY ? 0.f : fast_exp2(mk[i] - m), piece_at(i)[h * RS + D + 1], l);
+    float* row = piece_at(k) + h * RS;
+    const float own = row[D];
+    row[D + 2] = own == -INFINITY ? 0.f : fast_exp2(own - m);
+    row[D + 3] = m;
+    row[D + 4] = l;
+  }
+  __syncthreads();
+  int open_seg[2] = {-1, -1}, open_c0[2] = {0, 0}, open_n[2] = {0, 0};     // segments of several CTAs: the one that ends here, the one that begins here
+  for (uint32_t left = __ballot_sync(0xffffffffu, seg_l >= 0); left;) {
+    const int first = __ffs(left) - 1, seg = __shfl_sync(0xffffffffu, seg_l, first);
+    const uint32_t group = __shfl_sync(0xffffffffu, group_l, first);
+    left &= ~group;
     const int sq = seg / HH, hh = seg - sq * HH, tiles = pre[sq + 1] - pre[sq];
     const int s0 = pre[sq] * HH + hh * tiles, s1 = s0 + tiles;
     const bool complete = s0 >= a && s1 <= e;
-    const int heads = min(H, p.G - hh % HG * H);
-    float* joint = joints + (static_cast<long long>(blockIdx.x) * 2 + (s0 >= a)) * kDecodePieceFloats;
+    const int heads = min(H, p.G - hh % HG * H), which = s0 >= a;
+    float* joint = joints + (static_cast<long long>(blockIdx.x) * 2 + which) * kDecodePieceFloats;
     for (int y = threadIdx.x; y < heads * (D / 4); y += kDecodeThreads) {
       const int h = y / (D / 4), d4 = y % (D / 4);
-      float m = -INFINITY, l = 0.f;
       float4 o = make_float4(0.f, 0.f, 0.f, 0.f);
-      for (int k = i; k < j; ++k)
-        if (seg_of[k] == seg) m = fmaxf(m, piece_at(k)[h * RS + D]);
-      for (int k = i; k < j; ++k) {
-        if (seg_of[k] != seg) continue;
-        const float* src = piece_at(k) + h * RS;
-        const float f = src[D] == -INFINITY ? 0.f : fast_exp2(src[D] - m);
-        const float4 v = *reinterpret_cast<const float4*>(src + d4 * 4);
-        l = fmaf(f, src[D + 1], l);
-        o.x = fmaf(f, v.x, o.x); o.y = fmaf(f, v.y, o.y); o.z = fmaf(f, v.z, o.z); o.w = fmaf(f, v.w, o.w);
-      }
+#pragma unroll
+      for (int i = 0; i < P; ++i)
+        if (group >> i & 1u) {
+          const float* src = piece_at(i) + h * RS;
+          const float4 v = *reinterpret_cast<const float4*>(src + d4 * 4);
+          const float f = src[D + 2];
+          o.x = fmaf(f, v.x, o.x); o.y = fmaf(f, v.y, o.y); o.z = fmaf(f, v.z, o.z); o.w = fmaf(f, v.w, o.w);
+        }
+      const float m = piece_at(first)[h * RS + D + 3], l = piece_at(first)[h * RS + D + 4];
       if (complete) {
         give(sq, hh, h, d4, o, m, l);
       } else {
@@ -1030,36 +1052,77 @@ __global__ void __launch_bounds__(DecodeShape<T, D, I8>::template warps<NT>() * 
         if (d4 == 0) *reinterpret_cast<float2*>(joint + h * RS + D) = make_float2(m, l);
       }
     }
-    i = j;
-    if (complete) continue;
-    // A segment of several CTAs: the one that comes last joins them all, in their order.
-    // (boundaries c0 + 1 .. c1 lie inside the segment and have stayed there)
-    const int c0 = (s0 + near + per) / per - 1, c1 = (s1 - near - 1) / per;
-    __threadfence();
-    __syncthreads();
-    if (threadIdx.x == 0) {
-      s_last = atomicAdd(counters + seg, 1) == c1 - c0;
-      if (s_last) counters[seg] = 0;                         // as it was found
+    if (!complete) {                                         // boundaries c0 + 1 .. c1 lie inside the segment and have stayed there
+      const int c0 = (s0 + near + per) / per - 1, c1 = (s1 - near - 1) / per;
+      if (which) { open_seg[1] = seg; open_c0[1] = c0; open_n[1] = c1 - c0 + 1; } else { open_seg[0] = seg; open_c0[0] = c0; open_n[0] = c1 - c0 + 1; }
     }
+  }
+  if (open_seg[0] < 0 && open_seg[1] < 0) return;
+  // Of the CTAs of a segment the one that comes last joins them all, in their order.
+  __syncthreads();
+  if (threadIdx.x < 2) {
+    const int seg = threadIdx.x ? open_seg[1] : open_seg[0], n = threadIdx.x ? open_n[1] : open_n[0];
+    int last_one = 0;
+    if (seg >= 0) {
+      __threadfence();                                       // (what the block has written before the barrier goes first)
+      last_one = atomicAdd(counters + seg, 1) == n - 1;
+      if (last_one) counters[seg] = 0;                       // as it was found
+      __threadfence();
+    }
+    s_last[threadIdx.x] = last_one;
+  }
+  __syncthreads();
+#pragma unroll 1
+  for (int w = 0; w < 2; ++w) {
+    if (!s_last[w]) continue;
+    const int seg = w ? open_seg[1] : open_seg[0], c0 = w ? open_c0[1] : open_c0[0], n = w ? open_n[1] : open_n[0];
+    const int sq = seg / HH, hh = seg - sq * HH, heads = min(H, p.G - hh % HG * H);
+    // (shared memory of the rings, which nobody uses any more: factors [n][heads], joined (m, l) [heads], sums of parts)
+    float2* ml = reinterpret_cast<float2*>(smem_b);
+    float2* all = ml + kDecodeMaxCtas * H;
+    float4* sums = reinterpret_cast<float4*>(all + H);
+    auto piece = [&](int k) { return joints + (static_cast<long long>(c0 + k) * 2 + (k == 0)) * kDecodePieceFloats; };
+    for (int y = threadIdx.x; y < n * heads; y += kDecodeThreads) ml[y] = __ldcg(reinterpret_cast<const float2*>(piece(y / heads) + y % heads * RS + D));
     __syncthreads();
-    if (!s_last) continue;
-    __threadfence();
-    for (int y = threadIdx.x; y < heads * (D / 4); y += kDecodeThreads) {
-      const int h = y / (D / 4), d4 = y % (D / 4);
+    for (int h = warp; h < heads; h += kDecodeWarps) {
       float m = -INFINITY, l = 0.f;
-      float4 o = make_float4(0.f, 0.f, 0.f, 0.f);
-#pragma unroll 8
-      for (int k = c0; k <= c1; ++k) {
-        const float* src = joints + (static_cast<long long>(k) * 2 + (k == c0)) * kDecodePieceFloats + h * RS;
-        const float4 v = __ldcg(reinterpret_cast<const float4*>(src + d4 * 4));
-        const float2 ml = __ldcg(reinterpret_cast<const float2*>(src + D));
-        const float mn = fmaxf(m, ml.x), f0 = mn == -INFINITY ? 0.f : fast_exp2(m - mn), f1 = mn == -INFINITY ? 0.f : fast_exp2(ml.x - mn);
-        m = mn;
-        l = fmaf(f1, ml.y, l * f0);
-        o.x = fmaf(f1, v.x, o.x * f0); o.y = fmaf(f1, v.y, o.y * f0); o.z = fmaf(f1, v.z, o.z * f0); o.w = fmaf(f1, v.w, o.w * f0);
+      for (int k = lane; k < n; k += 32) m = fmaxf(m, ml[k * heads + h].x);
+#pragma unroll
+      for (int o = 16; o > 0; o >>= 1) m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, o));
+      for (int k = lane; k < n; k += 32) {
+        const float2 x = ml[k * heads + h];
+        const float f = x.x == -INFINITY ? 0.f : fast_exp2(x.x - m);
+        l = fmaf(f, x.y, l);
+        ml[k * heads + h].x = f;
       }
-      give(sq, hh, h, d4, o, m, l);
+#pragma unroll
+      for (int o = 16; o > 0; o >>= 1) l += __shfl_xor_sync(0xffffffffu, l, o);
+      if (lane == 0) all[h] = make_float2(m, l);
     }
+    __syncthreads();
+    const int rows = heads * (D / 4), parts = max(1, min(kDecodeThreads / rows, n));
+    for (int y0 = 0; y0 < rows; y0 += kDecodeThreads) {      // (one round unless there are more rows than threads; then one part)
+      const int y = y0 + threadIdx.x % (parts > 1 ? rows : kDecodeThreads), part = parts > 1 ? threadIdx.x / rows : 0;
+      const int h = y / (D / 4), d4 = y % (D / 4);
+      const bool mine = y < rows && part < parts;
+      float4 o = make_float4(0.f, 0.f, 0.f, 0.f);
+      if (mine) {
+#pragma unroll 8
+        for (int k = part; k < n; k += parts) {
+          const float4 v = __ldcg(reinterpret_cast<const float4*>(piece(k) + h * RS + d4 * 4));
+          const float f = ml[k * heads + h].x;
+          o.x = fmaf(f, v.x, o.x); o.y = fmaf(f, v.y, o.y); o.z = fmaf(f, v.z, o.z); o.w = fmaf(f, v.w, o.w);
+        }
+      }
+      if (parts > 1) {
+        if (mine && part > 0) sums[(part - 1) * rows + y] = o;
+        __syncthreads();
+        if (mine && part == 0)
+          for (int i = 0; i < parts - 1; ++i) { const float4 v = sums[i * rows + y]; o.x += v.x; o.y += v.y; o.z += v.z; o.w += v.w; }
+      }
+      if (mine && part == 0) give(sq, hh, h, d4, o, all[h].x, all[h].y);
+    }
+    __syncthreads();
   }
 }
 
