@@ -1082,6 +1082,19 @@ __global__ void __launch_bounds__(DecodeShape<T, D, I8>::template warps<NT>() * 
     float2* all = ml + kDecodeMaxCtas * H;
     float4* sums = reinterpret_cast<float4*>(all + H);
     auto piece = [&](int k) { return joints + (static_cast<long long>(c0 + k) * 2 + (k == 0)) * kDecodePieceFloats; };
+    const int rows = heads * (D / 4), parts = max(1, min(kDecodeThreads / rows, n));
+    const int part = parts > 1 ? threadIdx.x / rows : 0;
+    constexpr int kBatch = 8;                                // loads of a thread on their way: a trip to L2 takes 900 cycles
+    float4 v[kBatch];
+    auto fetch = [&](int y, int k0) {
+#pragma unroll
+      for (int i = 0; i < kBatch; ++i) {
+        const int k = k0 + i * parts;
+        v[i] = y < rows && k < n ? __ldcg(reinterpret_cast<const float4*>(piece(k) + y / (D / 4) * RS + y % (D / 4) * 4)) : make_float4(0.f, 0.f, 0.f, 0.f);
+      }
+    };
+    const int y_first = parts > 1 ? (part < parts ? static_cast<int>(threadIdx.x) - part * rows : rows) : threadIdx.x;
+    fetch(y_first, part);                                    // (before the factors are known)
     for (int y = threadIdx.x; y < n * heads; y += kDecodeThreads) ml[y] = __ldcg(reinterpret_cast<const float2*>(piece(y / heads) + y % heads * RS + D));
     __syncthreads();
     for (int h = warp; h < heads; h += kDecodeWarps) {
@@ -1100,27 +1113,24 @@ __global__ void __launch_bounds__(DecodeShape<T, D, I8>::template warps<NT>() * 
       if (lane == 0) all[h] = make_float2(m, l);
     }
     __syncthreads();
-    const int rows = heads * (D / 4), parts = max(1, min(kDecodeThreads / rows, n));
-    for (int y0 = 0; y0 < rows; y0 += kDecodeThreads) {      // (one round unless there are more rows than threads; then one part)
-      const int y = y0 + threadIdx.x % (parts > 1 ? rows : kDecodeThreads), part = parts > 1 ? threadIdx.x / rows : 0;
-      const int h = y / (D / 4), d4 = y % (D / 4);
-      const bool mine = y < rows && part < parts;
+    for (int y = y_first, round = 0; round * kDecodeThreads < rows; ++round, y += kDecodeThreads) {   // (one round, or one part)
+      const int h = min(y, rows - 1) / (D / 4), d4 = y % (D / 4);
       float4 o = make_float4(0.f, 0.f, 0.f, 0.f);
-      if (mine) {
-#pragma unroll 8
-        for (int k = part; k < n; k += parts) {
-          const float4 v = __ldcg(reinterpret_cast<const float4*>(piece(k) + h * RS + d4 * 4));
-          const float f = ml[k * heads + h].x;
-          o.x = fmaf(f, v.x, o.x); o.y = fmaf(f, v.y, o.y); o.z = fmaf(f, v.z, o.z); o.w = fmaf(f, v.w, o.w);
+      for (int k0 = part; k0 < n; k0 += kBatch * parts) {
+        if (round > 0 || k0 > part) fetch(y, k0);
+#pragma unroll
+        for (int i = 0; i < kBatch; ++i) {
+          const float f = ml[min(k0 + i * parts, n - 1) * heads + h].x;      // (times zero behind the last)
+          o.x = fmaf(f, v[i].x, o.x); o.y = fmaf(f, v[i].y, o.y); o.z = fmaf(f, v[i].z, o.z); o.w = fmaf(f, v[i].w, o.w);
         }
       }
       if (parts > 1) {
-        if (mine && part > 0) sums[(part - 1) * rows + y] = o;
+        if (y < rows && part > 0) sums[(part - 1) * rows + y] = o;
         __syncthreads();
-        if (mine && part == 0)
-          for (int i = 0; i < parts - 1; ++i) { const float4 v = sums[i * rows + y]; o.x += v.x; o.y += v.y; o.z += v.z; o.w += v.w; }
+        if (y < rows && part == 0)
+          for (int i = 0; i < parts - 1; ++i) { const float4 x = sums[i * rows + y]; o.x += x.x; o.y += x.y; o.z += x.z; o.w += x.w; }
       }
-      if (mine && part == 0) give(sq, hh, h, d4, o, all[h].x, all[h].y);
+      if (y < rows && part == 0) give(sq, hh, h, d4, o, all[h].x, all[h].y);
     }
     __syncthreads();
   }
