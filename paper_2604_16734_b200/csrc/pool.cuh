@@ -514,7 +514,7 @@ struct Decoder {
 #pragma unroll
     for (int n = 0; n < NT; ++n)
 #pragma unroll
-      for (int i = 0; i < 4; ++i) part[0][n][i] = part[1][n][i] = 0.f;
+      for (int i = 0; i < 4; ++i) { part[0][n][i] = I8 && S::QP == 1 ? -qb[n][i & 1] : 0.f; part[1][n][i] = 0.f; }
 #pragma unroll
     for (int j = 0; j < S::CK; ++j) {
       const uint4 w0 = *reinterpret_cast<const uint4*>(keys + key_at(r, c * 16 + j * 64)), w1 = *reinterpret_cast<const uint4*>(keys + key_at(r + 8, c * 16 + j * 64));
@@ -559,7 +559,7 @@ struct Decoder {
   template <int N>
   __device__ __forceinline__ void tile(const uint8_t* stage, const int (&lim)[2]) {
     const int lane = threadIdx.x & 31, r = lane >> 2, c = lane & 3;
-    constexpr float kGrow = 8.f, kRoom = 7.f;
+    constexpr float kGrow = 8.f, kRoom = 7.f;                // (m2 has kRoom taken off)
     float x[N][NT][4], y[N][NT][4], lv[N][2], top = -INFINITY, top2 = -INFINITY;
 #pragma unroll
     for (int t = 0; t < N; ++t) {
@@ -574,7 +574,6 @@ struct Decoder {
       for (int n = 0; n < NT; ++n)
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
-          if constexpr (I8 && S::QP == 1) x[t][n][i] -= qb[n][i & 1];
           x[t][n][i] *= I8 ? hf[n][i & 1] * ks[i >> 1] : hf[n][i & 1];
         }
       if (__builtin_expect(lim[t] < 16, 0)) {                // behind the end: nothing, whatever the zeros there gave
@@ -596,7 +595,7 @@ struct Decoder {
           if constexpr (I8) { y[t][n][i] = d + (lv[t][i >> 1] - m2[n][i & 1]); top2 = fmaxf(top2, y[t][n][i]); }
         }
     // A reference moves only when a score is more than 2^8 above it (or it is the first), for all heads at once.
-    if (__builtin_expect(__any_sync(0xffffffffu, top > kGrow || (I8 && top2 > kGrow)), 0)) {
+    if (__builtin_expect(__any_sync(0xffffffffu, top > kGrow || (I8 && top2 > kGrow + kRoom)), 0)) {
 #pragma unroll
       for (int n = 0; n < NT; ++n)
 #pragma unroll
@@ -616,7 +615,7 @@ struct Decoder {
             for (int t = 0; t < N; ++t) b = fmaxf(b, fmaxf((x[t][n][i] - mn) + lv[t][0], (x[t][n][i + 2] - mn) + lv[t][1]));
 #pragma unroll
             for (int o = 4; o < 32; o <<= 1) b = fmaxf(b, __shfl_xor_sync(0xffffffffu, b, o));
-            const float was = m2[n][i] + shift, mn2 = fmaxf(fmaxf(was, b), -1e30f);
+            const float was = m2[n][i] + shift, mn2 = fmaxf(fmaxf(was, b - kRoom), -1e30f);
             fo = fast_exp2(was - mn2);
             m2[n][i] = mn2;
 #pragma unroll
@@ -636,7 +635,7 @@ struct Decoder {
         for (int i = 0; i < 4; ++i) {
           const float e = fast_exp2(x[t][n][i] - m[n][i & 1]);
           l[n][i & 1] += e;
-          x[t][n][i] = I8 ? fast_exp2(y[t][n][i] + kRoom) : e;
+          x[t][n][i] = I8 ? fast_exp2(y[t][n][i]) : e;
         }
       product(stage + VO + t * HB, x[t]);
     }
@@ -730,7 +729,7 @@ struct Decoder {
 #pragma unroll
         for (int o = 4; o < 32; o <<= 1) l[n][i] += __shfl_xor_sync(0xffffffffu, l[n][i], o);
         if constexpr (I8) {
-          const float f = m2[n][i] == -INFINITY ? 1.f : exp2f(m2[n][i] - 7.f);   // (no tile)
+          const float f = m2[n][i] == -INFINITY ? 1.f : exp2f(m2[n][i]);   // (no tile)
 #pragma unroll
           for (int u = 0; u < S::MT; ++u) { acc[n][u][i] *= f; acc[n][u][i + 2] *= f; }
         }
