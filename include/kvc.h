@@ -373,7 +373,7 @@ typedef struct {
   int n_seqs;
   long long n_tokens;  /* rows of q, k, v and out             */
   int n_items;         /* pieces of work                       */
-  int row_tiles;       /* row tiles per piece, or rows per piece on the CUDA cores (fp32) */
+  int row_tiles;       /* row tiles per piece (bf16), rows per piece (fp32)  */
   size_t item_bytes;   /* bytes of the items                   */
 } kvc_prompt_plan;
 int kvc_pool_plan(kvc_pool* pool, const int* lens, int n_seqs, kvc_prompt_plan* plan, void* items);

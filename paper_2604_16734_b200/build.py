@@ -11,7 +11,7 @@ HERE = os.path.dirname(os.path.abspath(__file__))
 CSRC = os.path.join(HERE, "csrc")
 LIB = os.path.join(HERE, "libkvc.so")
 SOURCES = ["kvc_api.cu", "pool_api.cu"]
-HEADERS = ["geom.cuh", "ptx.cuh", "kernels_cc.cuh", "kernels_tc.cuh", "compress.cuh", "pool.cuh", "prompt.cuh"]
+HEADERS = ["geom.cuh", "ptx.cuh", "kernels_cc.cuh", "kernels_tc.cuh", "compress.cuh", "pool.cuh", "prompt.cuh", "prompt_f32.cuh"]
 
 
 CALLS = os.path.join(HERE, "_pool_calls" + (sysconfig.get_config_var("EXT_SUFFIX") or ".so"))

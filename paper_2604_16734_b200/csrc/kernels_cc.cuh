@@ -56,10 +56,7 @@ struct AttnCc {
   static constexpr int kBytes = (BM * KS + kCcWarps * BM * PS + kCcWarps * kWarpFloats + 3 * kCcWarps * BM) * 4;
 };
 
-// PACKED: whole prompts of different lengths, one after the other; no cache, no append, S = 1.  A CTA takes an item of a list
-// (`cache` points at it: first token of the prompt, its tokens, row tile); p.q_ls and p.kv_ls are the strides of a token's rows in q
-// and in k / v, p.score_off is the address of the log-sum-exp rows (0: none).
-template <typename T, int D, int BM, bool PACKED = false>
+template <typename T, int D, int BM>
 __global__ void __launch_bounds__(kCcThreads, 1) attn_cc_kernel(const T* __restrict__ q, const T* __restrict__ k,
                                                                 const T* __restrict__ v, char* __restrict__ cache,
                                                                 T* __restrict__ out, char* __restrict__ ws, Geom p, int S) {
@@ -80,25 +77,18 @@ __global__ void __launch_bounds__(kCcThreads, 1) attn_cc_kernel(const T* __restr
   float* sL = sM + kCcWarps * BM;                           // [8][BM] row sums
   float* sA = sL + kCcWarps * BM;                           // [2][BM] merged maximum and sum
 
-  const int lin = blockIdx.y * gridDim.x + blockIdx.x;
-  const int layer = blockIdx.z, g = PACKED ? lin % gridDim.y : blockIdx.y;
+  const int layer = blockIdx.z, g = blockIdx.y;
   const int split = S > 1 ? static_cast<int>(cluster_ctarank()) : 0;
-  int4 item = make_int4(0, 0, 0, 0);
-  if constexpr (PACKED) {
-    item = reinterpret_cast<const int4*>(cache)[lin / gridDim.y];
-    p.n = item.y;
-  }
-  const int tile = PACKED ? item.z : static_cast<int>(gridDim.x) / S - 1 - static_cast<int>(blockIdx.x) / S;   // longest rows first
+  const int tile = static_cast<int>(gridDim.x) / S - 1 - static_cast<int>(blockIdx.x) / S;   // longest rows first
   const int row0 = tile * BM, rows = p.n * p.G;
   char* blob = cache + layer * p.cache_ls;
   T* Kc = reinterpret_cast<T*>(blob) + static_cast<long long>(g) * p.cap * D;
   T* Vc = reinterpret_cast<T*>(blob + p.v_off) + static_cast<long long>(g) * p.cap * D;
-  const long long in_stride = PACKED ? p.kv_ls : static_cast<long long>(p.Hkv) * D;
-  const T* Kn = k + (PACKED ? item.x : layer) * p.kv_ls + static_cast<long long>(g) * D;
-  const T* Vn = v + (PACKED ? item.x : layer) * p.kv_ls + static_cast<long long>(g) * D;
-  const T* qb = q + (PACKED ? item.x : layer) * p.q_ls + static_cast<long long>(g) * p.G * D;
+  const long long in_stride = static_cast<long long>(p.Hkv) * D;
+  const T* Kn = k + layer * p.kv_ls + static_cast<long long>(g) * D;
+  const T* Vn = v + layer * p.kv_ls + static_cast<long long>(g) * D;
+  const T* qb = q + layer * p.q_ls + static_cast<long long>(g) * p.G * D;
   auto row_off = [&](int r) { return (static_cast<long long>(r / p.G) * p.Hq + r % p.G) * D; };   // row r of q / out
-  auto q_off = [&](int r) { return PACKED ? r / p.G * p.q_ls + static_cast<long long>(r % p.G) * D : row_off(r); };
 
   pdl_wait();                                               // the previous block's compaction is done with the cache
   // (after the wait: the score kernel reads the inputs and the old cache rows before its own)
@@ -124,12 +114,12 @@ __global__ void __launch_bounds__(kCcThreads, 1) attn_cc_kernel(const T* __restr
   int kt = split * kCcWarps + warp;
   for (int i = threadIdx.x; i < BM * CPR; i += kCcThreads) {
     const int r = i / CPR, c = i % CPR * EPC;
-    stage16<T>(sQ + r * KS + c, qb + q_off(min(row0 + r, rows - 1)) + c);
+    stage16<T>(sQ + r * KS + c, qb + row_off(min(row0 + r, rows - 1)) + c);
   }
   fetch(sK, KS, Kc, Kn, kt);
   fetch(sV, D, Vc, Vn, kt);
   // a0: warp w of CTA x copies tokens 8x + w, ...: one row of K and one of V each
-  for (int t = blockIdx.x * kCcWarps + warp; !PACKED && t < p.n; t += gridDim.x * kCcWarps) {
+  for (int t = blockIdx.x * kCcWarps + warp; t < p.n; t += gridDim.x * kCcWarps) {
     const long long dst = p.n_c + t;
     if (lane < CPR) {
       reinterpret_cast<uint4*>(Kc + dst * D)[lane] = reinterpret_cast<const uint4*>(Kn + t * in_stride)[lane];
@@ -264,14 +254,13 @@ __global__ void __launch_bounds__(kCcThreads, 1) attn_cc_kernel(const T* __restr
     sA[r] = ma; sA[BM + r] = sum;
   }
   __syncthreads();
-  T* ob = out + (PACKED ? static_cast<long long>(item.x) * p.Hq * D : layer * p.out_ls) + static_cast<long long>(g) * p.G * D;
-  float* lse = PACKED ? reinterpret_cast<float*>(p.score_off) + static_cast<long long>(item.x) * p.Hq + g * p.G
-                      : reinterpret_cast<float*>(ws_slot(ws, p, layer) + p.lse_off) + g * p.G;
+  T* ob = out + layer * p.out_ls + static_cast<long long>(g) * p.G * D;
+  float* lse = reinterpret_cast<float*>(ws_slot(ws, p, layer) + p.lse_off) + g * p.G;
   auto write = [&](int r, int c, float4 o, float mx, float sum) {
     if (row0 + r >= rows) return;
     const float inv = 1.f / sum;
     store4<T>(ob + row_off(row0 + r) + c * 4, make_float4(o.x * inv, o.y * inv, o.z * inv, o.w * inv));
-    if (c == 0 && (!PACKED || p.score_off)) lse[static_cast<long long>((row0 + r) / p.G) * p.Hq + (row0 + r) % p.G] = (mx + log2f(sum)) * 0.6931471805599453f;
+    if (c == 0) lse[static_cast<long long>((row0 + r) / p.G) * p.Hq + (row0 + r) % p.G] = (mx + log2f(sum)) * 0.6931471805599453f;
   };
 #pragma unroll 1
   for (int i = threadIdx.x; i < BM * D / 4; i += kCcThreads) {

@@ -14,9 +14,9 @@
 #include <new>
 
 #include "geom.cuh"
-#include "kernels_cc.cuh"
 #include "pool.cuh"
 #include "prompt.cuh"
+#include "prompt_f32.cuh"
 
 typedef CUresult (*EncodeTiledFn)(CUtensorMap*, CUtensorMapDataType, cuuint32_t, void*, const cuuint64_t*,
                                   const cuuint64_t*, const cuuint32_t*, const cuuint32_t*, CUtensorMapInterleave,
@@ -255,11 +255,9 @@ extern "C" int kvc_pool_decode(kvc_pool* c, const void* q, long long q_stride, c
 }
 
 // ------------------------------------------------------------------------------------------------ prompts
-// Pieces of work, longest first.  A row tile is 128 / G tokens on the tensor cores (bf16), two to a piece; kPromptRowsCc rows of
-// (token, head) on the CUDA cores (fp32).
+// Pieces of work, longest first.  A row tile is 128 / G tokens on the tensor cores (bf16), two to a piece; kRowsF32 rows of
+// (token, head) in fp32.
 using kvc::PromptItem;
-
-static const int kPromptRowsCc = 32;
 
 extern "C" int kvc_pool_plan(kvc_pool* c, const int* lens, int n_seqs, kvc_prompt_plan* plan, void* items) {
   if (!live(c)) return KVC_ESTATE;
@@ -272,7 +270,7 @@ extern "C" int kvc_pool_plan(kvc_pool* c, const int* lens, int n_seqs, kvc_promp
     tokens += lens[i];
   }
   if (tokens * c->cfg.n_q_heads > 0x7fffffffll) return fail(c, KVC_EINVAL, "%lld tokens of %d query heads: 2^31 rows or more", tokens, c->cfg.n_q_heads);
-  const int R = f32 ? kPromptRowsCc : 2;
+  const int R = f32 ? kvc::kRowsF32 : 2;
   long long n_items = 0;
   for (int i = 0; i < n_seqs; ++i) {
     const long long t = f32 ? ((long long)lens[i] * G + R - 1) / R : (lens[i] + TOK - 1) / TOK;
@@ -330,13 +328,13 @@ static cudaError_t launch_prompt_tc(const kvc_pool* c, const CUtensorMap (&m)[3]
 }
 
 template <int D>
-static cudaError_t launch_prompt_cc(const kvc_pool* c, const void* q, const void* k, const void* v, const kvc_prompt_plan* plan,
-                                    const void* items, void* ws, void* out, const kvc::Geom& g, cudaStream_t st) {
-  using L = kvc::AttnCc<D, kPromptRowsCc>;
+static cudaError_t launch_prompt_f32(const kvc_pool* c, const void* q, long long q_stride, const void* k, const void* v, long long kv_stride,
+                                     const kvc_prompt_plan* plan, const void* items, void* out, float* lse, cudaStream_t st) {
+  constexpr int smem = kvc::F32Prompt<D>::kBytes;
   static bool attr_set[kMaxDevices] = {};
-  if (cudaError_t e = opt_in_smem(kvc::attn_cc_kernel<float, D, kPromptRowsCc, true>, L::kBytes, attr_set, c->cfg.device)) return e;
-  kvc::attn_cc_kernel<float, D, kPromptRowsCc, true><<<dim3(plan->n_items, g.Hkv), kvc::kCcThreads, L::kBytes, st>>>(
-      (const float*)q, (const float*)k, (const float*)v, (char*)const_cast<void*>(items), (float*)out, (char*)ws, g, 1);
+  if (cudaError_t e = opt_in_smem(kvc::prompt_f32_kernel<D>, smem, attr_set, c->cfg.device)) return e;
+  kvc::prompt_f32_kernel<D><<<dim3(plan->n_items, c->geom.Hkv), kvc::kThreadsF32, smem, st>>>(
+      (const float*)q, q_stride, (const float*)k, (const float*)v, kv_stride, (const PromptItem*)items, c->geom.G, c->geom.Hq, c->geom.scale_log2, (float*)out, lse);
   return cudaGetLastError();
 }
 
@@ -347,7 +345,7 @@ extern "C" int kvc_pool_prompt(kvc_pool* c, const void* q, long long q_stride, c
   if (!plan || !workspace) return fail(c, KVC_EINVAL, "null pointer argument");
   const bool f32 = cf.dtype == KVC_F32;
   if (plan->n_tokens < 0 || plan->n_items < 0 || (long long)plan->n_items * cf.n_kv_heads > 0x7fffffffll || plan->n_tokens * cf.n_q_heads > 0x7fffffffll || plan->item_bytes != sizeof(PromptItem) * (size_t)plan->n_items ||
-      plan->row_tiles != (f32 ? kPromptRowsCc : 2))
+      plan->row_tiles != (f32 ? kvc::kRowsF32 : 2))
     return fail(c, KVC_EINVAL, "the plan is not one of this pool's");
   if (plan->n_tokens > 0 && (!q || !k || !v || !items || !out)) return fail(c, KVC_EINVAL, "null pointer argument");
   if (!aligned16(q) || !aligned16(k) || !aligned16(v) || !aligned16(items) || !aligned16(workspace) || !aligned16(out) || (reinterpret_cast<uintptr_t>(lse) & 3))
@@ -358,15 +356,8 @@ extern "C" int kvc_pool_prompt(kvc_pool* c, const void* q, long long q_stride, c
   if (plan->n_tokens == 0) return KVC_OK;
   cudaError_t e;
   if (f32) {
-    kvc::Geom g;
-    memset(&g, 0, sizeof(g));
-    g.G = c->geom.G; g.Hq = cf.n_q_heads; g.Hkv = cf.n_kv_heads; g.d = cf.head_dim; g.nl = 1;
-    g.scale_log2 = c->geom.scale_log2;
-    g.q_ls = q_stride; g.kv_ls = kv_stride;
-    g.score_off = (long long)reinterpret_cast<intptr_t>(lse);
-    g.wait_limit_k = kvc::kDefaultWaitLimitK;
-    e = cf.head_dim == 128 ? launch_prompt_cc<128>(c, q, k, v, plan, items, workspace, out, g, (cudaStream_t)stream)
-                           : launch_prompt_cc<64>(c, q, k, v, plan, items, workspace, out, g, (cudaStream_t)stream);
+    e = cf.head_dim == 128 ? launch_prompt_f32<128>(c, q, q_stride, k, v, kv_stride, plan, items, out, lse, (cudaStream_t)stream)
+                           : launch_prompt_f32<64>(c, q, q_stride, k, v, kv_stride, plan, items, out, lse, (cudaStream_t)stream);
   } else {
     if (!c->encode) {
       void* fn = nullptr;

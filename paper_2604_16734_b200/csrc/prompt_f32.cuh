@@ -1,0 +1,223 @@
+// Causal attention of whole prompts of different lengths, packed one after the other (fp32).
+#pragma once
+#include "pool.cuh"
+#include "prompt.cuh"
+#include "ptx.cuh"
+
+namespace kvc {
+
+// A CTA takes kRowsF32 rows of (token, head) of a prompt and kv-head; two warps share sixteen of them and halve every tile of keys (so
+// that a matrix instruction's way is covered by another warp's: one warp took 6300 cycles a tile of 64 keys, 3200 of them busy):
+//   S = Q K^T and O += P V with mma.sync m16n8k8 on TF32 parts (x = hi + lo, hi hi + hi lo + lo hi: 2^-21 and below, sums in fp32).
+// That is 92 of the 277 TFLOP/s that the instruction reaches here, against 67 for fused multiply-adds two at a time.  The order of a
+// contraction is free: a lane (r, c) = (lane / 4, lane % 4) takes whole 16-byte pieces of Q and K rows, and of V rows 2c and 2c + 1 -- the
+// keys whose scores it holds in the accumulators of S, so that probabilities go on as they are.  K and V tiles are shared by the
+// CTA's warps (cp.async, two stages; rows behind the prompt's end become zeros without being read) in the exchanged order of the
+// decode kernel's stages: no bank conflicts.
+// Bound: the matrix pipe for long prompts, a CTA's chain of key tiles for short ones.
+// grid (pieces, Hkv), pieces with the most keys first, block 256, dynamic smem F32Prompt::kBytes.
+static constexpr int kRowsF32 = 64, kThreadsF32 = 256;
+template <int D> struct F32Prompt {
+  static constexpr int KT = 64;                             // keys per tile
+  static constexpr int ROWB = D * 4, TILE = KT * ROWB, kBytes = 4 * TILE;   // K and V, twice
+  static __device__ __forceinline__ int key_at(int row, int byte) { return row * ROWB + (byte ^ ((row & 1) << 6)); }
+  static __device__ __forceinline__ int value_at(int row, int byte) { return row * ROWB + (byte ^ (((row >> 1) & 3) << 5)); }
+};
+
+template <int D>
+__global__ void __launch_bounds__(kThreadsF32) prompt_f32_kernel(const float* __restrict__ q, long long q_stride, const float* __restrict__ k,
+                                                                 const float* __restrict__ v, long long kv_stride,
+                                                                 const PromptItem* __restrict__ items, int G, int Hq, float scale_log2,
+                                                                 float* __restrict__ out, float* __restrict__ lse) {
+  using F = F32Prompt<D>;
+  constexpr int KT = F::KT, NK = KT / 16, PIECES = D / 4, NQ = D / 16;
+  extern __shared__ __align__(128) uint8_t smem_b[];
+  const int lin = blockIdx.y * gridDim.x + blockIdx.x, g = lin % gridDim.y;
+  const int4 it = *reinterpret_cast<const int4*>(items + lin / gridDim.y);
+  const int warp = threadIdx.x >> 5 & 3, half = threadIdx.x >> 7, lane = threadIdx.x & 31, r = lane >> 2, c = lane & 3;
+  const int rows = it.y * G, row0 = it.z * kRowsF32;
+  const int kv_end = (min(row0 + kRowsF32, rows) - 1) / G + 1;             // keys that the CTA's last row sees
+  const int n_tiles = (kv_end + KT - 1) / KT;
+  const float* kp = k + it.x * kv_stride + static_cast<long long>(g) * D;
+  const float* vp = v + it.x * kv_stride + static_cast<long long>(g) * D;
+
+  auto load = [&](int t) {
+    if (t < n_tiles) {
+      const uint32_t to = smem_u32(smem_b) + (t & 1) * 2 * F::TILE;
+#pragma unroll
+      for (int i = 0; i < KT * PIECES / kThreadsF32; ++i) {
+        const int x = i * kThreadsF32 + threadIdx.x, row = x / PIECES, piece = x % PIECES, key = t * KT + row;
+        const long long at = min(key, kv_end - 1) * kv_stride + piece * 4;
+        const int bytes = key < kv_end ? 16 : 0;
+        copy16(to + F::key_at(row, piece * 16), kp + at, bytes);
+        copy16(to + F::TILE + F::value_at(row, piece * 16), vp + at, bytes);
+      }
+    }
+    cp_async_commit();
+  };
+  load(0);
+
+  // rows r and r + 8 of the warp's sixteen
+  int tok[2];
+  float4 qr[2][NQ];
+#pragma unroll
+  for (int i = 0; i < 2; ++i) {
+    const int row = min(row0 + warp * 16 + r + 8 * i, rows - 1);
+    tok[i] = row / G;
+    const float* src = q + (it.x + tok[i]) * q_stride + static_cast<long long>(g * G + row % G) * D + c * 4;
+#pragma unroll
+    for (int j = 0; j < NQ; ++j) qr[i][j] = *reinterpret_cast<const float4*>(src + j * 16);
+  }
+  const int tok_last = min(row0 + warp * 16 + 15, rows - 1) / G;           // the last token of the warp's rows
+  float o[D / 8][4], m[2] = {-INFINITY, -INFINITY}, l[2] = {0.f, 0.f};
+#pragma unroll
+  for (int i = 0; i < D / 8; ++i)
+#pragma unroll
+    for (int j = 0; j < 4; ++j) o[i][j] = 0.f;
+
+  for (int t = 0; t < n_tiles; ++t) {
+    load(t + 1);
+    cp_async_wait<1>();
+    __syncthreads();
+    const uint8_t* sk = smem_b + (t & 1) * 2 * F::TILE + half * (F::TILE / 2);
+    const uint8_t* sv = sk + F::TILE;
+    const int key0 = t * KT + half * (KT / 2);               // this warp's first key
+    if (key0 <= tok_last) {                                // (a warp whose rows see none of the tile passes)
+      float s[NK][4];
+#pragma unroll
+      for (int n = 0; n < NK; ++n)
+#pragma unroll
+        for (int i = 0; i < 4; ++i) s[n][i] = 0.f;
+#pragma unroll
+      for (int j = 0; j < NQ; ++j) {
+        uint32_t hi[2][4], lo[2][4];                         // the two steps' fragments of Q
+        {
+          const float4 a = qr[0][j], b = qr[1][j];
+          split_tf32(__float_as_uint(a.x), hi[0][0], lo[0][0]); split_tf32(__float_as_uint(b.x), hi[0][1], lo[0][1]);
+          split_tf32(__float_as_uint(a.y), hi[0][2], lo[0][2]); split_tf32(__float_as_uint(b.y), hi[0][3], lo[0][3]);
+          split_tf32(__float_as_uint(a.z), hi[1][0], lo[1][0]); split_tf32(__float_as_uint(b.z), hi[1][1], lo[1][1]);
+          split_tf32(__float_as_uint(a.w), hi[1][2], lo[1][2]); split_tf32(__float_as_uint(b.w), hi[1][3], lo[1][3]);
+        }
+#pragma unroll
+        for (int n = 0; n < NK; ++n) {
+          const uint4 w = *reinterpret_cast<const uint4*>(sk + F::key_at(n * 8 + r, c * 16 + j * 64));
+          const uint32_t x[4] = {w.x, w.y, w.z, w.w};
+#pragma unroll
+          for (int h = 0; h < 2; ++h) {
+            uint32_t bh0, bl0, bh1, bl1;
+            split_tf32(x[2 * h], bh0, bl0);
+            split_tf32(x[2 * h + 1], bh1, bl1);
+            mma_tf32(s[n], lo[h], bh0, bh1);
+            mma_tf32(s[n], hi[h], bl0, bl1);
+            mma_tf32(s[n], hi[h], bh0, bh1);
+          }
+        }
+      }
+      // columns 8 n + 2 c, + 1 of rows r (0, 1) and r + 8 (2, 3)
+      const bool masked = key0 + KT / 2 > tok[0] + 1;          // (tok[0] <= tok[1])
+      float mx[2] = {-INFINITY, -INFINITY};
+#pragma unroll
+      for (int n = 0; n < NK; ++n)
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          s[n][i] *= scale_log2;
+          if (masked && key0 + 8 * n + 2 * c + (i & 1) > tok[i >> 1]) s[n][i] = -INFINITY;
+          mx[i >> 1] = fmaxf(mx[i >> 1], s[n][i]);
+        }
+      float f[2];
+#pragma unroll
+      for (int i = 0; i < 2; ++i) {
+        mx[i] = fmaxf(mx[i], __shfl_xor_sync(0xffffffffu, mx[i], 1));
+        mx[i] = fmaxf(mx[i], __shfl_xor_sync(0xffffffffu, mx[i], 2));
+        const float mn = fmax3(m[i], mx[i], -1e30f);         // (a row that sees none of the tile: differences stay numbers)
+        f[i] = fast_exp2(m[i] - mn);
+        m[i] = mn;
+        l[i] *= f[i];
+      }
+#pragma unroll
+      for (int n = 0; n < NK; ++n)
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          s[n][i] = fast_exp2(s[n][i] - m[i >> 1]);
+          l[i >> 1] += s[n][i];
+        }
+      if (__any_sync(0xffffffffu, f[0] != 1.f || f[1] != 1.f)) {
+#pragma unroll
+        for (int i = 0; i < D / 8; ++i) { o[i][0] *= f[0]; o[i][1] *= f[0]; o[i][2] *= f[1]; o[i][3] *= f[1]; }
+      }
+      // eight keys at a time: step c is key 2 c, step c + 4 key 2 c + 1
+#pragma unroll
+      for (int n = 0; n < NK; ++n) {
+        uint32_t hi[4], lo[4];
+        split_tf32(__float_as_uint(s[n][0]), hi[0], lo[0]); split_tf32(__float_as_uint(s[n][2]), hi[1], lo[1]);
+        split_tf32(__float_as_uint(s[n][1]), hi[2], lo[2]); split_tf32(__float_as_uint(s[n][3]), hi[3], lo[3]);
+#pragma unroll
+        for (int d = 0; d < D / 32; ++d) {
+          const uint4 w0 = *reinterpret_cast<const uint4*>(sv + F::value_at(n * 8 + 2 * c, r * 16 + d * 128));
+          const uint4 w1 = *reinterpret_cast<const uint4*>(sv + F::value_at(n * 8 + 2 * c + 1, r * 16 + d * 128));
+          const uint32_t x0[4] = {w0.x, w0.y, w0.z, w0.w}, x1[4] = {w1.x, w1.y, w1.z, w1.w};
+#pragma unroll
+          for (int e = 0; e < 4; ++e) {                      // channels 32 d + 4 r + e
+            uint32_t bh0, bl0, bh1, bl1;
+            split_tf32(x0[e], bh0, bl0);
+            split_tf32(x1[e], bh1, bl1);
+            mma_tf32(o[d * 4 + e], lo, bh0, bh1);
+            mma_tf32(o[d * 4 + e], hi, bl0, bl1);
+            mma_tf32(o[d * 4 + e], hi, bh0, bh1);
+          }
+        }
+      }
+    }
+    __syncthreads();                                         // the tile after next goes over this one
+  }
+  // the halves' results: the second one's go through shared memory, a thread's where the same lane of the first reads them
+#pragma unroll
+  for (int i = 0; i < 2; ++i) {
+    l[i] += __shfl_xor_sync(0xffffffffu, l[i], 1);
+    l[i] += __shfl_xor_sync(0xffffffffu, l[i], 2);
+  }
+  float4* other = reinterpret_cast<float4*>(smem_b) + (threadIdx.x & 127);
+  if (half) {
+#pragma unroll
+    for (int i = 0; i < D / 8; ++i) other[i * 128] = make_float4(o[i][0], o[i][1], o[i][2], o[i][3]);
+    other[D / 8 * 128] = make_float4(m[0], m[1], l[0], l[1]);
+  }
+  __syncthreads();
+  if (half) return;
+  {
+    const float4 ml = other[D / 8 * 128];
+    const float om[2] = {ml.x, ml.y}, ol[2] = {ml.z, ml.w};
+    float f[2], fo[2];
+#pragma unroll
+    for (int i = 0; i < 2; ++i) {                            // (the first half always has the key 0)
+      const float mn = fmaxf(m[i], om[i]);
+      f[i] = fast_exp2(m[i] - mn);
+      fo[i] = fast_exp2(om[i] - mn);
+      m[i] = mn;
+      l[i] = fmaf(f[i], l[i], fo[i] * ol[i]);
+    }
+#pragma unroll
+    for (int i = 0; i < D / 8; ++i) {
+      const float4 x = other[i * 128];
+      o[i][0] = fmaf(f[0], o[i][0], fo[0] * x.x); o[i][1] = fmaf(f[0], o[i][1], fo[0] * x.y);
+      o[i][2] = fmaf(f[1], o[i][2], fo[1] * x.z); o[i][3] = fmaf(f[1], o[i][3], fo[1] * x.w);
+    }
+  }
+#pragma unroll
+  for (int i = 0; i < 2; ++i) {
+    const int row = row0 + warp * 16 + r + 8 * i;
+    if (row >= rows) continue;
+    const long long to = static_cast<long long>(it.x + tok[i]) * Hq + g * G + row % G;
+    const float inv = 1.f / l[i];
+#pragma unroll
+    for (int d = 0; d < D / 32; ++d)
+#pragma unroll
+      for (int j = 0; j < 2; ++j) {                          // channels 32 d + 8 c + 4 j ..
+        const int at = 2 * i + j;
+        *reinterpret_cast<float4*>(out + to * D + 32 * d + 8 * c + 4 * j) = make_float4(o[4 * d][at] * inv, o[4 * d + 1][at] * inv, o[4 * d + 2][at] * inv, o[4 * d + 3][at] * inv);
+      }
+    if (lse && c == 0) lse[to] = (m[i] + log2f(l[i])) * 0.6931471805599453f;
+  }
+}
+
+}  // namespace kvc
