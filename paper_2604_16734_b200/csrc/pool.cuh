@@ -333,11 +333,12 @@ __device__ __forceinline__ void mma_tf32(float* d, const uint32_t* a, uint32_t b
   asm volatile("mma.sync.aligned.m16n8k8.row.col.f32.tf32.tf32.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, {%0, %1, %2, %3};"
                : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3]) : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
 }
-// x = hi + lo in TF32 (eleven bits; the instruction drops those behind).  Both are rounded, not cut: cut parts are all off towards
-// zero, which adds up over a dot product (log-sum-exp of scores around 600: off by 6e-4 instead of below 1e-4).
+// x = hi + lo in TF32 (eleven bits; the instruction drops those behind).  hi is rounded, not cut: cut parts leave lo with x's sign, and
+// what is dropped adds up over a dot product (log-sum-exp of scores around 600: off by 6e-4 instead of below 1e-4).  lo has either
+// sign then, and may be cut.
 __device__ __forceinline__ void split_tf32(uint32_t x, uint32_t& hi, uint32_t& lo) {
   hi = (x + 0x1000u) & 0xffffe000u;
-  lo = __float_as_uint(__uint_as_float(x) - __uint_as_float(hi)) + 0x1000u;
+  lo = __float_as_uint(__uint_as_float(x) - __uint_as_float(hi));
 }
 __device__ __forceinline__ void mma_3tf32(float* d, const uint32_t* x, uint32_t b0, uint32_t b1) {
   uint32_t hi[4], lo[4], bh0, bl0, bh1, bl1;

@@ -255,8 +255,8 @@ extern "C" int kvc_pool_decode(kvc_pool* c, const void* q, long long q_stride, c
 }
 
 // ------------------------------------------------------------------------------------------------ prompts
-// Pieces of work, longest first.  A row tile is 128 / G tokens on the tensor cores (bf16), two to a piece; kRowsF32 rows of
-// (token, head) in fp32.
+// Pieces of work, longest first.  A row tile is 128 / G tokens on the tensor cores (bf16), two to a piece; 64 or 32
+// rows of (token, head) in fp32.
 using kvc::PromptItem;
 
 extern "C" int kvc_pool_plan(kvc_pool* c, const int* lens, int n_seqs, kvc_prompt_plan* plan, void* items) {
@@ -270,7 +270,12 @@ extern "C" int kvc_pool_plan(kvc_pool* c, const int* lens, int n_seqs, kvc_promp
     tokens += lens[i];
   }
   if (tokens * c->cfg.n_q_heads > 0x7fffffffll) return fail(c, KVC_EINVAL, "%lld tokens of %d query heads: 2^31 rows or more", tokens, c->cfg.n_q_heads);
-  const int R = f32 ? kvc::kRowsF32 : 2;
+  int R = 2;
+  if (f32) {                                                 // (the rule's two sides are measured at the kernel)
+    long long pieces = 0;
+    for (int i = 0; i < n_seqs; ++i) pieces += ((long long)lens[i] * G + 63) / 64;
+    R = pieces * c->cfg.n_kv_heads > kvc::kNumSMs ? 64 : 32;
+  }
   long long n_items = 0;
   for (int i = 0; i < n_seqs; ++i) {
     const long long t = f32 ? ((long long)lens[i] * G + R - 1) / R : (lens[i] + TOK - 1) / TOK;
@@ -327,13 +332,13 @@ static cudaError_t launch_prompt_tc(const kvc_pool* c, const CUtensorMap (&m)[3]
   return cudaGetLastError();
 }
 
-template <int D>
+template <int D, int RG>
 static cudaError_t launch_prompt_f32(const kvc_pool* c, const void* q, long long q_stride, const void* k, const void* v, long long kv_stride,
                                      const kvc_prompt_plan* plan, const void* items, void* out, float* lse, cudaStream_t st) {
-  constexpr int smem = kvc::F32Prompt<D>::kBytes;
+  constexpr int smem = kvc::F32Prompt<D, RG>::kBytes;
   static bool attr_set[kMaxDevices] = {};
-  if (cudaError_t e = opt_in_smem(kvc::prompt_f32_kernel<D>, smem, attr_set, c->cfg.device)) return e;
-  kvc::prompt_f32_kernel<D><<<dim3(plan->n_items, c->geom.Hkv), kvc::kThreadsF32, smem, st>>>(
+  if (cudaError_t e = opt_in_smem(kvc::prompt_f32_kernel<D, RG>, smem, attr_set, c->cfg.device)) return e;
+  kvc::prompt_f32_kernel<D, RG><<<dim3(plan->n_items, c->geom.Hkv), kvc::kThreadsF32, smem, st>>>(
       (const float*)q, q_stride, (const float*)k, (const float*)v, kv_stride, (const PromptItem*)items, c->geom.G, c->geom.Hq, c->geom.scale_log2, (float*)out, lse);
   return cudaGetLastError();
 }
@@ -345,7 +350,7 @@ extern "C" int kvc_pool_prompt(kvc_pool* c, const void* q, long long q_stride, c
   if (!plan || !workspace) return fail(c, KVC_EINVAL, "null pointer argument");
   const bool f32 = cf.dtype == KVC_F32;
   if (plan->n_tokens < 0 || plan->n_items < 0 || (long long)plan->n_items * cf.n_kv_heads > 0x7fffffffll || plan->n_tokens * cf.n_q_heads > 0x7fffffffll || plan->item_bytes != sizeof(PromptItem) * (size_t)plan->n_items ||
-      plan->row_tiles != (f32 ? kvc::kRowsF32 : 2))
+      (f32 ? plan->row_tiles != 64 && plan->row_tiles != 32 : plan->row_tiles != 2))
     return fail(c, KVC_EINVAL, "the plan is not one of this pool's");
   if (plan->n_tokens > 0 && (!q || !k || !v || !items || !out)) return fail(c, KVC_EINVAL, "null pointer argument");
   if (!aligned16(q) || !aligned16(k) || !aligned16(v) || !aligned16(items) || !aligned16(workspace) || !aligned16(out) || (reinterpret_cast<uintptr_t>(lse) & 3))
@@ -356,8 +361,9 @@ extern "C" int kvc_pool_prompt(kvc_pool* c, const void* q, long long q_stride, c
   if (plan->n_tokens == 0) return KVC_OK;
   cudaError_t e;
   if (f32) {
-    e = cf.head_dim == 128 ? launch_prompt_f32<128>(c, q, q_stride, k, v, kv_stride, plan, items, out, lse, (cudaStream_t)stream)
-                           : launch_prompt_f32<64>(c, q, q_stride, k, v, kv_stride, plan, items, out, lse, (cudaStream_t)stream);
+    auto run = [&](auto launcher) { return launcher(c, q, q_stride, k, v, kv_stride, plan, items, out, lse, (cudaStream_t)stream); };
+    if (cf.head_dim == 128) e = plan->row_tiles == 64 ? run(launch_prompt_f32<128, 4>) : run(launch_prompt_f32<128, 2>);
+    else e = plan->row_tiles == 64 ? run(launch_prompt_f32<64, 4>) : run(launch_prompt_f32<64, 2>);
   } else {
     if (!c->encode) {
       void* fn = nullptr;

@@ -6,37 +6,39 @@
 
 namespace kvc {
 
-// A CTA takes kRowsF32 rows of (token, head) of a prompt and kv-head; two warps share sixteen of them and halve every tile of keys (so
-// that a matrix instruction's way is covered by another warp's: one warp took 6300 cycles a tile of 64 keys, 3200 of them busy):
+// A CTA takes 16 RG rows of (token, head) of a prompt and kv-head; 8 / RG warps share sixteen of them and part every tile of keys:
 //   S = Q K^T and O += P V with mma.sync m16n8k8 on TF32 parts (x = hi + lo, hi hi + hi lo + lo hi: 2^-21 and below, sums in fp32).
 // That is 92 of the 277 TFLOP/s that the instruction reaches here, against 67 for fused multiply-adds two at a time.  The order of a
 // contraction is free: a lane (r, c) = (lane / 4, lane % 4) takes whole 16-byte pieces of Q and K rows, and of V rows 2c and 2c + 1 -- the
 // keys whose scores it holds in the accumulators of S, so that probabilities go on as they are.  K and V tiles are shared by the
 // CTA's warps (cp.async, two stages; rows behind the prompt's end become zeros without being read) in the exchanged order of the
 // decode kernel's stages: no bank conflicts.
-// Bound: the matrix pipe for long prompts, a CTA's chain of key tiles for short ones.
+// Bound: the matrix pipe at 57 % (4 x 2048 tokens, 32 / 8 heads: 52 TFLOP/s at d = 64, 53 at d = 128), beside it taking numbers apart; a
+// CTA's chain of key tiles for short prompts.  RG = 4, or 2 where there are no more pieces than SMs: 576 tokens, 4 / 1 heads, d = 64
+// 16.4 us against 28.5, three prompts of 300, 20, 500, 8 / 2 heads, d = 128 28 against 49; 4 x 2048 tokens 1432 against 1333.
 // grid (pieces, Hkv), pieces with the most keys first, block 256, dynamic smem F32Prompt::kBytes.
-static constexpr int kRowsF32 = 64, kThreadsF32 = 256;
-template <int D> struct F32Prompt {
-  static constexpr int KT = 64;                             // keys per tile
+static constexpr int kThreadsF32 = 256;
+template <int D, int RG> struct F32Prompt {
+  static constexpr int ROWS = 16 * RG, PARTS = 8 / RG;
+  static constexpr int KT = D == 64 && RG == 2 ? 128 : 64;  // keys per tile
   static constexpr int ROWB = D * 4, TILE = KT * ROWB, kBytes = 4 * TILE;   // K and V, twice
   static __device__ __forceinline__ int key_at(int row, int byte) { return row * ROWB + (byte ^ ((row & 1) << 6)); }
   static __device__ __forceinline__ int value_at(int row, int byte) { return row * ROWB + (byte ^ (((row >> 1) & 3) << 5)); }
 };
 
-template <int D>
-__global__ void __launch_bounds__(kThreadsF32) prompt_f32_kernel(const float* __restrict__ q, long long q_stride, const float* __restrict__ k,
+template <int D, int RG>
+__global__ void __launch_bounds__(kThreadsF32, 1) prompt_f32_kernel(const float* __restrict__ q, long long q_stride, const float* __restrict__ k,
                                                                  const float* __restrict__ v, long long kv_stride,
                                                                  const PromptItem* __restrict__ items, int G, int Hq, float scale_log2,
                                                                  float* __restrict__ out, float* __restrict__ lse) {
-  using F = F32Prompt<D>;
-  constexpr int KT = F::KT, NK = KT / 16, PIECES = D / 4, NQ = D / 16;
+  using F = F32Prompt<D, RG>;
+  constexpr int KT = F::KT, KP = KT / F::PARTS, NK = KP / 8, PIECES = D / 4, NQ = D / 16;
   extern __shared__ __align__(128) uint8_t smem_b[];
   const int lin = blockIdx.y * gridDim.x + blockIdx.x, g = lin % gridDim.y;
   const int4 it = *reinterpret_cast<const int4*>(items + lin / gridDim.y);
-  const int warp = threadIdx.x >> 5 & 3, half = threadIdx.x >> 7, lane = threadIdx.x & 31, r = lane >> 2, c = lane & 3;
-  const int rows = it.y * G, row0 = it.z * kRowsF32;
-  const int kv_end = (min(row0 + kRowsF32, rows) - 1) / G + 1;             // keys that the CTA's last row sees
+  const int warp = (threadIdx.x >> 5) % RG, part = (threadIdx.x >> 5) / RG, lane = threadIdx.x & 31, r = lane >> 2, c = lane & 3;
+  const int rows = it.y * G, row0 = it.z * F::ROWS;
+  const int kv_end = (min(row0 + F::ROWS, rows) - 1) / G + 1;             // keys that the CTA's last row sees
   const int n_tiles = (kv_end + KT - 1) / KT;
   const float* kp = k + it.x * kv_stride + static_cast<long long>(g) * D;
   const float* vp = v + it.x * kv_stride + static_cast<long long>(g) * D;
@@ -79,9 +81,9 @@ __global__ void __launch_bounds__(kThreadsF32) prompt_f32_kernel(const float* __
     load(t + 1);
     cp_async_wait<1>();
     __syncthreads();
-    const uint8_t* sk = smem_b + (t & 1) * 2 * F::TILE + half * (F::TILE / 2);
+    const uint8_t* sk = smem_b + (t & 1) * 2 * F::TILE + part * (KP * F::ROWB);
     const uint8_t* sv = sk + F::TILE;
-    const int key0 = t * KT + half * (KT / 2);               // this warp's first key
+    const int key0 = t * KT + part * KP;                     // this warp's first key
     if (key0 <= tok_last) {                                // (a warp whose rows see none of the tile passes)
       float s[NK][4];
 #pragma unroll
@@ -98,23 +100,27 @@ __global__ void __launch_bounds__(kThreadsF32) prompt_f32_kernel(const float* __
           split_tf32(__float_as_uint(a.z), hi[1][0], lo[1][0]); split_tf32(__float_as_uint(b.z), hi[1][1], lo[1][1]);
           split_tf32(__float_as_uint(a.w), hi[1][2], lo[1][2]); split_tf32(__float_as_uint(b.w), hi[1][3], lo[1][3]);
         }
+        uint4 w[NK];
 #pragma unroll
-        for (int n = 0; n < NK; ++n) {
-          const uint4 w = *reinterpret_cast<const uint4*>(sk + F::key_at(n * 8 + r, c * 16 + j * 64));
-          const uint32_t x[4] = {w.x, w.y, w.z, w.w};
+        for (int n = 0; n < NK; ++n) w[n] = *reinterpret_cast<const uint4*>(sk + F::key_at(n * 8 + r, c * 16 + j * 64));
 #pragma unroll
-          for (int h = 0; h < 2; ++h) {
-            uint32_t bh0, bl0, bh1, bl1;
-            split_tf32(x[2 * h], bh0, bl0);
-            split_tf32(x[2 * h + 1], bh1, bl1);
-            mma_tf32(s[n], lo[h], bh0, bh1);
-            mma_tf32(s[n], hi[h], bl0, bl1);
-            mma_tf32(s[n], hi[h], bh0, bh1);
+        for (int h = 0; h < 2; ++h) {                        // (products of one sum are NK instructions apart)
+          uint32_t bh[NK][2], bl[NK][2];
+#pragma unroll
+          for (int n = 0; n < NK; ++n) {
+            split_tf32(h ? w[n].z : w[n].x, bh[n][0], bl[n][0]);
+            split_tf32(h ? w[n].w : w[n].y, bh[n][1], bl[n][1]);
           }
+#pragma unroll
+          for (int n = 0; n < NK; ++n) mma_tf32(s[n], lo[h], bh[n][0], bh[n][1]);
+#pragma unroll
+          for (int n = 0; n < NK; ++n) mma_tf32(s[n], hi[h], bl[n][0], bl[n][1]);
+#pragma unroll
+          for (int n = 0; n < NK; ++n) mma_tf32(s[n], hi[h], bh[n][0], bh[n][1]);
         }
       }
       // columns 8 n + 2 c, + 1 of rows r (0, 1) and r + 8 (2, 3)
-      const bool masked = key0 + KT / 2 > tok[0] + 1;          // (tok[0] <= tok[1])
+      const bool masked = key0 + KP > tok[0] + 1;          // (tok[0] <= tok[1])
       float mx[2] = {-INFINITY, -INFINITY};
 #pragma unroll
       for (int n = 0; n < NK; ++n)
@@ -156,40 +162,46 @@ __global__ void __launch_bounds__(kThreadsF32) prompt_f32_kernel(const float* __
           const uint4 w0 = *reinterpret_cast<const uint4*>(sv + F::value_at(n * 8 + 2 * c, r * 16 + d * 128));
           const uint4 w1 = *reinterpret_cast<const uint4*>(sv + F::value_at(n * 8 + 2 * c + 1, r * 16 + d * 128));
           const uint32_t x0[4] = {w0.x, w0.y, w0.z, w0.w}, x1[4] = {w1.x, w1.y, w1.z, w1.w};
+          uint32_t bh[4][2], bl[4][2];
 #pragma unroll
-          for (int e = 0; e < 4; ++e) {                      // channels 32 d + 4 r + e
-            uint32_t bh0, bl0, bh1, bl1;
-            split_tf32(x0[e], bh0, bl0);
-            split_tf32(x1[e], bh1, bl1);
-            mma_tf32(o[d * 4 + e], lo, bh0, bh1);
-            mma_tf32(o[d * 4 + e], hi, bl0, bl1);
-            mma_tf32(o[d * 4 + e], hi, bh0, bh1);
-          }
+          for (int e = 0; e < 4; ++e) { split_tf32(x0[e], bh[e][0], bl[e][0]); split_tf32(x1[e], bh[e][1], bl[e][1]); }
+          // channels 32 d + 4 r + e
+#pragma unroll
+          for (int e = 0; e < 4; ++e) mma_tf32(o[d * 4 + e], lo, bh[e][0], bh[e][1]);
+#pragma unroll
+          for (int e = 0; e < 4; ++e) mma_tf32(o[d * 4 + e], hi, bl[e][0], bl[e][1]);
+#pragma unroll
+          for (int e = 0; e < 4; ++e) mma_tf32(o[d * 4 + e], hi, bh[e][0], bh[e][1]);
         }
       }
     }
     __syncthreads();                                         // the tile after next goes over this one
   }
-  // the halves' results: the second one's go through shared memory, a thread's where the same lane of the first reads them
+  // the parts' results: those of all but the first go through shared memory, a thread's where the same lane of the first reads them
 #pragma unroll
   for (int i = 0; i < 2; ++i) {
     l[i] += __shfl_xor_sync(0xffffffffu, l[i], 1);
     l[i] += __shfl_xor_sync(0xffffffffu, l[i], 2);
   }
-  float4* other = reinterpret_cast<float4*>(smem_b) + (threadIdx.x & 127);
-  if (half) {
+  constexpr int kGroup = RG * 32, kHeld = (D / 8 + 1) * kGroup;   // threads of a part, pieces that they leave
+  static_assert((F::PARTS - 1) * kHeld * 16 <= F::kBytes);
+  float4* held = reinterpret_cast<float4*>(smem_b) + threadIdx.x % kGroup;
+  if (part) {
+    float4* mine = held + (part - 1) * kHeld;
 #pragma unroll
-    for (int i = 0; i < D / 8; ++i) other[i * 128] = make_float4(o[i][0], o[i][1], o[i][2], o[i][3]);
-    other[D / 8 * 128] = make_float4(m[0], m[1], l[0], l[1]);
+    for (int i = 0; i < D / 8; ++i) mine[i * kGroup] = make_float4(o[i][0], o[i][1], o[i][2], o[i][3]);
+    mine[D / 8 * kGroup] = make_float4(m[0], m[1], l[0], l[1]);
   }
   __syncthreads();
-  if (half) return;
-  {
-    const float4 ml = other[D / 8 * 128];
+  if (part) return;
+#pragma unroll 1
+  for (int x = 0; x < F::PARTS - 1; ++x) {
+    const float4* other = held + x * kHeld;
+    const float4 ml = other[D / 8 * kGroup];
     const float om[2] = {ml.x, ml.y}, ol[2] = {ml.z, ml.w};
     float f[2], fo[2];
 #pragma unroll
-    for (int i = 0; i < 2; ++i) {                            // (the first half always has the key 0)
+    for (int i = 0; i < 2; ++i) {                            // (the first part always has the key 0)
       const float mn = fmaxf(m[i], om[i]);
       f[i] = fast_exp2(m[i] - mn);
       fo[i] = fast_exp2(om[i] - mn);
@@ -198,9 +210,9 @@ __global__ void __launch_bounds__(kThreadsF32) prompt_f32_kernel(const float* __
     }
 #pragma unroll
     for (int i = 0; i < D / 8; ++i) {
-      const float4 x = other[i * 128];
-      o[i][0] = fmaf(f[0], o[i][0], fo[0] * x.x); o[i][1] = fmaf(f[0], o[i][1], fo[0] * x.y);
-      o[i][2] = fmaf(f[1], o[i][2], fo[1] * x.z); o[i][3] = fmaf(f[1], o[i][3], fo[1] * x.w);
+      const float4 y = other[i * kGroup];
+      o[i][0] = fmaf(f[0], o[i][0], fo[0] * y.x); o[i][1] = fmaf(f[0], o[i][1], fo[0] * y.y);
+      o[i][2] = fmaf(f[1], o[i][2], fo[1] * y.z); o[i][3] = fmaf(f[1], o[i][3], fo[1] * y.w);
     }
   }
 #pragma unroll
