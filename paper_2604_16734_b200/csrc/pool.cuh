@@ -1,5 +1,10 @@
 // Kernels of the page pool: rows into pages and back (as they are or in 8 bits), and attention of one new token per sequence
 // over its pages.
+//
+// All of them are launched with programmatic stream serialization: they are brought up while the kernel before them ends, wait for
+// its end before they touch memory, and then let the next one be brought up (one after another, against plain launches: 192 tokens
+// written 4.1 -> 2.8 us, one short sequence decoded 8.2 -> 6.3, 1225 + 24 tokens 10.8 -> 9.5, 64 sequences of 845 in 8 bits
+// 101.6 -> 100.7).  What a kernel reads is no `const __restrict__`: such loads may be moved in front of the wait.
 #pragma once
 #include "geom.cuh"
 #include "kernels_cc.cuh"
@@ -12,7 +17,9 @@ struct PoolGeom {
   int Hq, Hkv, G, n_pages;
   int ps_log2;                     // page size = 1 << ps_log2
   float scale_log2;                // softmax scale times log2(e)
-  int min_keys;                    // decode: fewest keys (of all segments) that a CTA gets, in whole tiles
+  // Decode: fewest keys (of all segments) that a CTA gets, in whole tiles.  256, against 128 and 512: one sequence of 1000, 32 / 8
+  // heads, d = 128 10.2, 10.3, 11.4 us; sixteen of 100 - 700 12.0, 12.0, 14.6; four of 1500, 28 / 4 heads 13.2, 12.7, 14.3.
+  int min_keys;
   long long v_off, ks_off, vs_off; // byte offsets inside a blob of V, K scales, V scales (K is at 0)
   long long joints_off;            // byte offset in the workspace of the pieces of segments that span CTAs
 };
@@ -143,13 +150,15 @@ __device__ __forceinline__ void put_codes(char* codes, float* scales, uint32_t d
 
 // grid ceil(n / (kRows * kWriteRows)) * Hkv, block 256
 template <typename T, int D, bool I8>
-__global__ void __launch_bounds__(kPoolThreads) pool_write_kernel(const T* __restrict__ k, const T* __restrict__ v, long long ts,
-                                                                  long long hs, const long long* __restrict__ slots, unsigned n,
+__global__ void __launch_bounds__(kPoolThreads) pool_write_kernel(const T* k, const T* v, long long ts,
+                                                                  long long hs, const long long* slots, unsigned n,
                                                                   char* __restrict__ blob, char* __restrict__ ws, PoolGeom p) {
   using R = RowShape<T, D>;
   const int l = threadIdx.x % R::kLanes;
   const unsigned h = blockIdx.x % p.Hkv, t0 = blockIdx.x / p.Hkv * (R::kRows * kWriteRows) + threadIdx.x / R::kLanes;
   const long long at = h * hs + l * R::N;
+  pdl_wait();
+  pdl_launch_dependents();
   uint4 kr[kWriteRows][2], vr[kWriteRows][2];
   uint32_t dst[kWriteRows];
 #pragma unroll
@@ -194,7 +203,7 @@ __device__ __forceinline__ uint4 from_codes(const uint32_t* c, float s) {
 
 // grid ceil(n / (kRows * kReadRows)) * Hkv, block 256
 template <typename T, int D, bool I8>
-__global__ void __launch_bounds__(kPoolThreads) pool_read_kernel(const char* __restrict__ blob, const long long* __restrict__ slots,
+__global__ void __launch_bounds__(kPoolThreads) pool_read_kernel(const char* blob, const long long* slots,
                                                                  unsigned n, T* __restrict__ k, T* __restrict__ v, long long ts,
                                                                  long long hs, char* __restrict__ ws, PoolGeom p) {
   using R = RowShape<T, D>;
@@ -204,6 +213,8 @@ __global__ void __launch_bounds__(kPoolThreads) pool_read_kernel(const char* __r
   const long long at = h * hs + l * N;
   uint32_t kr[kReadRows][2][W], vr[kReadRows][2][W];
   float sk[kReadRows], sv[kReadRows];
+  pdl_wait();
+  pdl_launch_dependents();
 #pragma unroll
   for (int i = 0; i < kReadRows; ++i) {
     const unsigned t = t0 + i * R::kRows;
@@ -309,7 +320,7 @@ struct DecodeShape {
   template <int N> static __host__ __device__ constexpr int warps() {
     return F32 && D == 128 ? 5 : N == 2 ? 8 : I8 ? 8 : D == 128 ? 6 : F32 ? 6 : 8;
   }
-  template <int N> static __host__ __device__ constexpr int near() { return 98304 / stage<N>(); }
+  template <int N> static __host__ __device__ constexpr int near() { return 98304 / stage<N>(); }   // (tiles; at its use)
   template <int N> static __host__ __device__ constexpr int stages() {
     const int n = (kDecodeSmem / warps<N>() / 128 * 128 - piece<N>() - OWN) / stage<N>();
     return n < 6 ? n : 6;
@@ -746,10 +757,10 @@ struct Decoder {
 
 // Pieces are joined as o = sum_i 2^(m_i - m) o_i, l likewise, m the largest m_i.  A piece: [heads][decode_row(D)].
 template <typename T, int D, bool I8, int NT>
-__global__ void __launch_bounds__(DecodeShape<T, D, I8>::template warps<NT>() * 32, 1) pool_decode_kernel(const T* __restrict__ q, long long q_stride,
-                                                                     const T* __restrict__ k_new, const T* __restrict__ v_new,
-                                                                     long long kv_stride, const int* __restrict__ table,
-                                                                     int table_stride, const int* __restrict__ lens, int n_seqs,
+__global__ void __launch_bounds__(DecodeShape<T, D, I8>::template warps<NT>() * 32, 1) pool_decode_kernel(const T* q, long long q_stride,
+                                                                     const T* k_new, const T* v_new,
+                                                                     long long kv_stride, const int* table,
+                                                                     int table_stride, const int* lens, int n_seqs,
                                                                      char* blob, char* __restrict__ ws, T* __restrict__ out,
                                                                      float* __restrict__ lse, PoolGeom p) {
   using S = DecodeShape<T, D, I8>;
@@ -776,6 +787,8 @@ __global__ void __launch_bounds__(DecodeShape<T, D, I8>::template warps<NT>() * 
   const int room = static_cast<int>((static_cast<long long>(table_stride) << p.ps_log2) - (k_new ? 1 : 0));
   if (threadIdx.x < kDecodeWarps * 2) s_seg[threadIdx.x >> 1][threadIdx.x & 1] = -1;
   if (threadIdx.x == 0) pre[0] = 0;
+  pdl_wait();
+  pdl_launch_dependents();
   int sum = 0;
   for (int i0 = 0; i0 < n_seqs; i0 += kDecodeThreads) {
     const int i = i0 + threadIdx.x;
@@ -798,8 +811,10 @@ __global__ void __launch_bounds__(DecodeShape<T, D, I8>::template warps<NT>() * 
   }
   const int total = sum * HH;
   const int per = max((total + static_cast<int>(gridDim.x) - 1) / static_cast<int>(gridDim.x), p.min_keys / TK);
-  // Where the ranges are short, a boundary moves to an end of its segment that is near: joining pieces across CTAs costs as much time
-  // as the loads of kNear tiles.
+  // Where the ranges are short, a boundary moves to an end of its segment that is near: joining pieces across CTAs costs about 3 us,
+  // as much as the loads of kNear tiles (96 KB).  Left out: one sequence of 2000, 28 / 4 heads, d = 128 13.0 -> 17.0 us, sixteen of
+  // 100 - 700, 32 / 8 heads in 8 bits 12.0 -> 17.0; twice as far 14.0, 12.0; half as far 11.7, 13.8, and one of 8000, 32 / 8 heads
+  // 13.6 -> 16.4.  (Where no boundary is near an end, the search costs 0.2 - 0.5 us.)
   constexpr int kNear = S::template near<NT>();
   const int near = per <= 4 * kNear ? kNear : 0;
   auto sequence_of = [&](int x) {                            // the sequence that holds tile x: the last whose tiles begin at or before it

@@ -142,6 +142,25 @@ extern "C" int kvc_pool_status(kvc_pool* c, void* workspace, void* stream) {
   return KVC_OK;
 }
 
+// Launches with programmatic stream serialization: a kernel may be brought up while the one before it ends, and waits for its end
+// (griddepcontrol.wait) before it touches memory.
+template <typename... P, typename... A>
+static cudaError_t launch(void (*kernel)(P...), dim3 grid, int threads, int smem, void* stream, A... args) {
+  cudaLaunchAttribute at;
+  memset(&at, 0, sizeof at);
+  at.id = cudaLaunchAttributeProgrammaticStreamSerialization;
+  at.val.programmaticStreamSerializationAllowed = 1;
+  cudaLaunchConfig_t lc;
+  memset(&lc, 0, sizeof lc);
+  lc.gridDim = grid;
+  lc.blockDim = dim3(threads);
+  lc.dynamicSmemBytes = smem;
+  lc.stream = (cudaStream_t)stream;
+  lc.attrs = &at;
+  lc.numAttrs = 1;
+  return cudaLaunchKernelEx(&lc, kernel, args...);
+}
+
 // What kvc_pool_write and kvc_pool_read check alike.
 static int check_rows(kvc_pool* c, const void* k, const void* v, long long ts, long long hs, const void* slots, long long n,
                       const void* blob, const void* ws) {
@@ -183,9 +202,8 @@ extern "C" int kvc_pool_write(kvc_pool* c, const void* k, const void* v, long lo
   const cudaError_t e = by_shape(c, [&](auto t, auto d, auto i8) {
     using T = decltype(t);
     constexpr int D = decltype(d)::value, per = kvc::RowShape<T, D>::kRows * kvc::kWriteRows;
-    kvc::pool_write_kernel<T, D, decltype(i8)::value><<<(unsigned)((n + per - 1) / per) * cf.n_kv_heads, kvc::kPoolThreads, 0, (cudaStream_t)stream>>>(
-        (const T*)k, (const T*)v, token_stride, head_stride, slots, (unsigned)n, (char*)blob, (char*)workspace, c->geom);
-    return cudaGetLastError();
+    return launch(kvc::pool_write_kernel<T, D, decltype(i8)::value>, dim3((unsigned)((n + per - 1) / per) * cf.n_kv_heads), kvc::kPoolThreads, 0, stream,
+                  (const T*)k, (const T*)v, token_stride, head_stride, slots, (unsigned)n, (char*)blob, (char*)workspace, c->geom);
   });
   c->launches++;
   return check_cuda(c, e, "write launch");
@@ -200,9 +218,8 @@ extern "C" int kvc_pool_read(kvc_pool* c, const void* blob, const long long* slo
   const cudaError_t e = by_shape(c, [&](auto t, auto d, auto i8) {
     using T = decltype(t);
     constexpr int D = decltype(d)::value, per = kvc::RowShape<T, D>::kRows * kvc::kReadRows;
-    kvc::pool_read_kernel<T, D, decltype(i8)::value><<<(unsigned)((n + per - 1) / per) * cf.n_kv_heads, kvc::kPoolThreads, 0, (cudaStream_t)stream>>>(
-        (const char*)blob, slots, (unsigned)n, (T*)k, (T*)v, token_stride, head_stride, (char*)workspace, c->geom);
-    return cudaGetLastError();
+    return launch(kvc::pool_read_kernel<T, D, decltype(i8)::value>, dim3((unsigned)((n + per - 1) / per) * cf.n_kv_heads), kvc::kPoolThreads, 0, stream,
+                  (const char*)blob, slots, (unsigned)n, (T*)k, (T*)v, token_stride, head_stride, (char*)workspace, c->geom);
   });
   c->launches++;
   return check_cuda(c, e, "read launch");
@@ -242,9 +259,8 @@ extern "C" int kvc_pool_decode(kvc_pool* c, const void* q, long long q_stride, c
       static bool attr_set[kMaxDevices] = {};
       if (cudaError_t x = opt_in_smem(kernel, base + (kvc::kDecodeMaxSeqs + 1) * 4 + kvc::kDecodeMaxSeqs, attr_set, cf.device)) return x;
       const int ctas = (int)std::max<long long>(1, std::min<long long>(kvc::kNumSMs, (most + c->geom.min_keys / 16 - 1) / (c->geom.min_keys / 16)));
-      kernel<<<ctas, W * 32, smem, (cudaStream_t)stream>>>((const T*)q, q_stride, (const T*)k_new, (const T*)v_new, kv_stride, table,
-                                                                        table_stride, lens, n_seqs, (char*)blob, (char*)workspace, (T*)out, lse, c->geom);
-      return cudaGetLastError();
+      return launch(kernel, dim3(ctas), W * 32, smem, stream, (const T*)q, q_stride, (const T*)k_new, (const T*)v_new, kv_stride, table, table_stride, lens,
+                    n_seqs, (char*)blob, (char*)workspace, (T*)out, lse, c->geom);
     };
     if constexpr (kvc::DecodeShape<T, D, I8>::NT == 2)
       if (c->geom.G > 8) return go(std::integral_constant<int, 2>());
@@ -328,8 +344,7 @@ static cudaError_t launch_prompt_tc(const kvc_pool* c, const CUtensorMap (&m)[3]
   g.wait_limit_k = kvc::kDefaultWaitLimitK;
   g.items = (const PromptItem*)items;
   g.lse = lse;
-  kvc::prompt_kernel<D><<<std::min(g.n_units, kvc::kNumSMs), kvc::kAttnThreads, smem, st>>>(m[0], m[1], m[2], (__nv_bfloat16*)out, (char*)ws, g);
-  return cudaGetLastError();
+  return launch(kvc::prompt_kernel<D>, dim3(std::min(g.n_units, kvc::kNumSMs)), kvc::kAttnThreads, smem, st, m[0], m[1], m[2], (__nv_bfloat16*)out, (char*)ws, g);
 }
 
 template <int D, int RG>
@@ -338,9 +353,8 @@ static cudaError_t launch_prompt_f32(const kvc_pool* c, const void* q, long long
   constexpr int smem = kvc::F32Prompt<D, RG>::kBytes;
   static bool attr_set[kMaxDevices] = {};
   if (cudaError_t e = opt_in_smem(kvc::prompt_f32_kernel<D, RG>, smem, attr_set, c->cfg.device)) return e;
-  kvc::prompt_f32_kernel<D, RG><<<dim3(plan->n_items, c->geom.Hkv), kvc::kThreadsF32, smem, st>>>(
-      (const float*)q, q_stride, (const float*)k, (const float*)v, kv_stride, (const PromptItem*)items, c->geom.G, c->geom.Hq, c->geom.scale_log2, (float*)out, lse);
-  return cudaGetLastError();
+  return launch(kvc::prompt_f32_kernel<D, RG>, dim3(plan->n_items, c->geom.Hkv), kvc::kThreadsF32, smem, st, (const float*)q, q_stride, (const float*)k,
+                (const float*)v, kv_stride, (const PromptItem*)items, c->geom.G, c->geom.Hq, c->geom.scale_log2, (float*)out, lse);
 }
 
 extern "C" int kvc_pool_prompt(kvc_pool* c, const void* q, long long q_stride, const void* k, const void* v, long long kv_stride,

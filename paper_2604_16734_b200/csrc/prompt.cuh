@@ -92,6 +92,8 @@ __global__ void __launch_bounds__(kAttnThreads, 1) prompt_kernel(const __grid_co
   __syncthreads();
   tc_fence_after_sync();
   const uint32_t tmem = sh.tmem_base;
+  pdl_wait();
+  pdl_launch_dependents();
 
   if (warp >= 8) {
     reg_dec<56>();

@@ -27,14 +27,16 @@ template <int D, int RG> struct F32Prompt {
 };
 
 template <int D, int RG>
-__global__ void __launch_bounds__(kThreadsF32, 1) prompt_f32_kernel(const float* __restrict__ q, long long q_stride, const float* __restrict__ k,
-                                                                 const float* __restrict__ v, long long kv_stride,
-                                                                 const PromptItem* __restrict__ items, int G, int Hq, float scale_log2,
+__global__ void __launch_bounds__(kThreadsF32, 1) prompt_f32_kernel(const float* q, long long q_stride, const float* k,
+                                                                 const float* v, long long kv_stride,
+                                                                 const PromptItem* items, int G, int Hq, float scale_log2,
                                                                  float* __restrict__ out, float* __restrict__ lse) {
   using F = F32Prompt<D, RG>;
   constexpr int KT = F::KT, KP = KT / F::PARTS, NK = KP / 8, PIECES = D / 4, NQ = D / 16;
   extern __shared__ __align__(128) uint8_t smem_b[];
   const int lin = blockIdx.y * gridDim.x + blockIdx.x, g = lin % gridDim.y;
+  pdl_wait();
+  pdl_launch_dependents();
   const int4 it = *reinterpret_cast<const int4*>(items + lin / gridDim.y);
   const int warp = (threadIdx.x >> 5) % RG, part = (threadIdx.x >> 5) / RG, lane = threadIdx.x & 31, r = lane >> 2, c = lane & 3;
   const int rows = it.y * G, row0 = it.z * F::ROWS;

@@ -485,6 +485,49 @@ def test_prompts_do_not_see_each_other(dtype, hq, hkv, lens, bad):
 
 
 # ---------------------------------------------------------------------------------------------------------------------- refusals
+@pytest.mark.parametrize("dtype,fmt", [(BF16, "plain"), (BF16, "int8"), (F32, "plain"), (F32, "int8")])
+def test_calls_that_follow_one_another_wait_for_one_another(dtype, fmt):
+    """Each call reads what the call before it writes, and writes over what that one reads, with nothing in between: the bits are
+    those of a run in which the host waits after every call."""
+    gen = torch.Generator(device="cuda").manual_seed(17)
+    heads, d, page, seqs, size = 4, 64, 32, 5, 700
+    pool = Pool(heads, heads, d, dtype, 256, page, fmt, max_seqs=seqs)
+    table = torch.randperm(256, generator=gen, device="cuda").int()[:seqs * 24].view(seqs, 24)
+    slots = torch.cat([pool.slots(table[i], size) for i in range(seqs)])
+    start = torch.randn(3, seqs * size, heads, d, generator=gen, device="cuda").to(dtype)
+    plans = [pool.plan([size] * seqs), pool.plan([1] * seqs), pool.plan([seqs * size])]
+    lens = torch.full((seqs,), size, dtype=torch.int32, device="cuda")
+
+    def run(wait):
+        x, y, z = start.clone()
+        pool.blob.zero_()
+        out, lse = torch.zeros_like(x), torch.zeros(seqs * size, heads, device="cuda")
+        few, few_lse = torch.zeros(seqs, heads, d, device="cuda", dtype=dtype), torch.zeros(seqs, heads, device="cuda")
+        torch.cuda.synchronize()
+        for step in range(12):
+            plan = plans[step % 3]
+            n = plan.n_tokens
+            calls = [lambda: pool.prompt(x[:n], y[:n], z[:n], plan, out[:n], lse[:n]),
+                     lambda: pool.write(0, out, z, slots),
+                     lambda: pool.read(0, slots, y, x),
+                     lambda: pool.decode(0, y[:seqs], table, lens, x[:seqs], y[:seqs], few, few_lse),
+                     lambda: pool.write(0, few, y[:seqs], slots[:seqs]),
+                     lambda: pool.read(0, slots[:seqs], x[:seqs], z[:seqs]),
+                     lambda: pool.decode(0, x[:seqs], table, lens, None, None, y[-seqs:], few_lse)]
+            for call in calls:
+                call()
+                if wait:
+                    torch.cuda.synchronize()
+        torch.cuda.synchronize()
+        return [t.clone() for t in (x, y, z, out, lse, few, few_lse, pool.blob)]
+
+    want = run(True)
+    assert bool(torch.isfinite(want[0].float()).all()) and pool.status() == KVC_OK
+    for _ in range(5):
+        for a, b in zip(run(False), want):
+            assert torch.equal(a.view(torch.uint8), b.view(torch.uint8))
+
+
 def test_refusals():
     pool = Pool(4, 2, 64, BF16, 3, 16, max_seqs=2)
     x, q = torch.zeros(2, 2, 64, device="cuda", dtype=BF16), torch.zeros(2, 4, 64, device="cuda", dtype=BF16)
