@@ -272,8 +272,46 @@ extern "C" int kvc_pool_decode(kvc_pool* c, const void* q, long long q_stride, c
 
 // ------------------------------------------------------------------------------------------------ prompts
 // Pieces of work, longest first.  A row tile is 128 / G tokens on the tensor cores (bf16), two to a piece; 64 or 32
-// rows of (token, head) in fp32.
+// rows of (token, head) in fp32.  In bf16 the units (piece, kv-head) are dealt out here, in the layout that the kernel reads.
 using kvc::PromptItem;
+
+static long long plan_bytes(const kvc_pool* c, long long n_items) {
+  if (c->cfg.dtype == KVC_F32) return n_items * (long long)sizeof(PromptItem);
+  const long long units = n_items * c->cfg.n_kv_heads;
+  return units * (long long)sizeof(PromptItem) + (std::min<long long>(units, kvc::kNumSMs) + 3) / 4 * 16;
+}
+
+// Units in the order of `items` (longest first, all kv-heads of a piece), each to the CTA with the least to do.
+static void deal(const PromptItem* items, long long n_items, int heads, int TOK, PromptItem* units) {
+  struct Load { long long keys; int cta; };
+  const long long n = n_items * heads;
+  const int C = (int)std::min<long long>(n, kvc::kNumSMs);
+  int* others = (int*)(units + n);                            // where each CTA's units but the first begin
+  const auto more = [](const Load& a, const Load& b) { return a.keys != b.keys ? a.keys > b.keys : a.cta > b.cta; };
+  long long at[kvc::kNumSMs];
+  int count[kvc::kNumSMs];
+  for (int pass = 0; pass < 2; ++pass) {                      // the first counts
+    Load heap[kvc::kNumSMs];
+    for (int i = 0; i < C; ++i) heap[i] = {0, i};
+    if (pass == 0) std::fill(count, count + C, 0);
+    long long next = C;
+    for (int i = 0; i < C && pass == 1; ++i) { at[i] = next; others[i] = (int)next; next += count[i] - 1; }
+    int given[kvc::kNumSMs] = {};
+    for (long long u = 0; u < n; ++u) {
+      const PromptItem& x = items[u / heads];
+      std::pop_heap(heap, heap + C, more);
+      Load& l = heap[C - 1];
+      if (pass == 0) count[l.cta]++;
+      else {
+        const int head = (int)(u % heads), k = given[l.cta]++;
+        units[k == 0 ? l.cta : at[l.cta]++] = {x.first, x.len, x.tile, k + 1 == count[l.cta] ? ~head : head};
+      }
+      l.keys += (std::min<long long>(x.len, ((long long)x.tile + 2) * TOK) + 127) / 128 + 1;   // (and a tile's time for its rows)
+      std::push_heap(heap, heap + C, more);
+    }
+  }
+  for (int i = C; i % 4; ++i) others[i] = 0;
+}
 
 extern "C" int kvc_pool_plan(kvc_pool* c, const int* lens, int n_seqs, kvc_prompt_plan* plan, void* items) {
   if (!live(c)) return KVC_ESTATE;
@@ -297,27 +335,32 @@ extern "C" int kvc_pool_plan(kvc_pool* c, const int* lens, int n_seqs, kvc_promp
     const long long t = f32 ? ((long long)lens[i] * G + R - 1) / R : (lens[i] + TOK - 1) / TOK;
     n_items += f32 ? t : (t + 1) / 2;
   }
-  if (n_items > 0x7fffffffll) return fail(c, KVC_EINVAL, "%lld pieces of work", n_items);
+  if (n_items * c->cfg.n_kv_heads > 0x7fffffffll) return fail(c, KVC_EINVAL, "%lld pieces of work", n_items);
   plan->n_seqs = n_seqs;
   plan->n_tokens = tokens;
   plan->n_items = (int)n_items;
   plan->row_tiles = R;
-  plan->item_bytes = sizeof(PromptItem) * (size_t)n_items;
-  if (!items) return KVC_OK;
-  PromptItem* it = (PromptItem*)items;
+  plan->item_bytes = (size_t)plan_bytes(c, n_items);
+  if (!items || n_items == 0) return KVC_OK;
+  PromptItem* it = f32 ? (PromptItem*)items : new (std::nothrow) PromptItem[n_items];
+  if (!it) return fail(c, KVC_EINVAL, "no host memory for %lld pieces of work", n_items);
   long long first = 0, n = 0;
   for (int i = 0; i < n_seqs; ++i) {
     const int t = f32 ? (int)(((long long)lens[i] * G + R - 1) / R) : (lens[i] + TOK - 1) / TOK;
     const int step = f32 ? 1 : R;
-    for (int k = 0; k < t; k += step) it[n++] = {(int)first, lens[i], k, std::min(step, t - k)};
+    for (int k = 0; k < t; k += step) it[n++] = {(int)first, lens[i], k, std::min(step, t - k)};   // (the last: row tiles, for the order)
     first += lens[i];
   }
   // longest first: a piece sees the keys up to its last token (ties keep their order, so a plan is the same every time)
   auto cost = [&](const PromptItem& x) {
-    const long long last = f32 ? std::min<long long>(x.len, ((long long)(x.tile + 1) * R + G - 1) / G) : std::min<long long>(x.len, (long long)(x.tile + x.tiles) * TOK);
-    return (last + 127) / 128 * (f32 ? 1 : 1 + x.tiles);
+    const long long last = f32 ? std::min<long long>(x.len, ((long long)(x.tile + 1) * R + G - 1) / G) : std::min<long long>(x.len, (long long)(x.tile + x.head) * TOK);
+    return (last + 127) / 128 * (f32 ? 1 : 1 + x.head);
   };
   std::stable_sort(it, it + n, [&](const PromptItem& a, const PromptItem& b) { return cost(a) > cost(b); });
+  if (!f32) {
+    deal(it, n, c->cfg.n_kv_heads, TOK, (PromptItem*)items);
+    delete[] it;
+  }
   return KVC_OK;
 }
 
@@ -363,7 +406,7 @@ extern "C" int kvc_pool_prompt(kvc_pool* c, const void* q, long long q_stride, c
   const kvc_pool_config& cf = c->cfg;
   if (!plan || !workspace) return fail(c, KVC_EINVAL, "null pointer argument");
   const bool f32 = cf.dtype == KVC_F32;
-  if (plan->n_tokens < 0 || plan->n_items < 0 || (long long)plan->n_items * cf.n_kv_heads > 0x7fffffffll || plan->n_tokens * cf.n_q_heads > 0x7fffffffll || plan->item_bytes != sizeof(PromptItem) * (size_t)plan->n_items ||
+  if (plan->n_tokens < 0 || plan->n_items < 0 || (long long)plan->n_items * cf.n_kv_heads > 0x7fffffffll || plan->n_tokens * cf.n_q_heads > 0x7fffffffll || plan->item_bytes != (size_t)plan_bytes(c, plan->n_items) ||
       (f32 ? plan->row_tiles != 64 && plan->row_tiles != 32 : plan->row_tiles != 2))
     return fail(c, KVC_EINVAL, "the plan is not one of this pool's");
   if (plan->n_tokens > 0 && (!q || !k || !v || !items || !out)) return fail(c, KVC_EINVAL, "null pointer argument");

@@ -8,10 +8,10 @@ namespace kvc {
 
 // A piece of work: two row tiles of a prompt for every kv-head.  A row tile is TOK = 128 / G tokens with the G query heads of a
 // kv-head beside each other (row = token * G + head), so keys and values are read once per kv-head.
-struct PromptItem { int first, len, tile, tiles; };        // first token and tokens of the prompt, first row tile, row tiles (1 or 2)
+struct PromptItem { int first, len, tile, head; };          // first token and tokens of the prompt, first row tile, kv-head (bf16: see unit_at)
 
 struct PromptGeom {
-  int G, Hq, Hkv, n_units;     // units: (piece, kv-head), kv-heads innermost, most key tiles first
+  int G, Hq, Hkv, n_units;     // units: (piece, kv-head)
   float scale_log2;
   int wait_limit_k;
   const PromptItem* items;
@@ -20,10 +20,13 @@ struct PromptGeom {
 
 // The arithmetic of a key tile is the block attention's with two row tiles (attn_tc_kernel: S = Q K^T and O += P V with tcgen05.mma,
 // accumulators in TMEM, a thread per row, exponentials in turns, lazy rescaling, S ahead of the softmax).  What differs is that a CTA
-// stays: it walks through units c, 2C - 1 - c, 2C + c, ... of C CTAs (there and back, since units are sorted by length), and its ring,
-// barriers and TMEM stay with it.  While the softmax warps write a unit's rows, the next unit's Q, keys and values are already on
-// their way and its first S is computed, so a unit costs its key tiles and about a microsecond.  With a CTA per unit (set-up, TMEM,
-// first loads and the last stores in nobody's shadow) it cost up to ten: 64 prompts of 128 tokens, 32 / 8 heads, d = 128 69 us.
+// stays: it walks through a list of units that the plan made -- each unit, longest first, goes to the CTA with the least to do, a unit
+// counted as its key tiles and one more for its rows -- and its ring, barriers and TMEM stay with it.  (Walked there and back over
+// units sorted by length, without lists: 8 prompts of 383 - 4096, 32 / 8 heads, d = 128 256 us instead of 250, 300 + 2000 + 40 + 900,
+// 28 / 4 heads 44 - 49 instead of 39 - 41.)  While the softmax warps write a unit's rows, the next unit's Q, keys and values are already
+// there and its first S is computed.  With a CTA per unit (set-up, TMEM, first loads and the last stores in nobody's shadow) a unit of
+// one key tile cost 9 us, in a list it costs 3.5: 470 cycles to its S, 1170 for its maximum, 1800 for its weights, 700 for P V, 2500 for
+// its rows.
 //   warps 0-3, 4-7  softmax of row tile A, B (216 registers); a warp's rows leave through a stage of its own, 64 columns at a time, as
 //                   whole lines (Q's shared memory is the next unit's by then; 32 bytes of 32 rows per store, straight from
 //                   registers, took 2500 cycles a unit, and so did TMA, whose second half waits for the first to leave)
@@ -32,7 +35,8 @@ struct PromptGeom {
 //   warp  11        zeroes the values behind a prompt's end in its last key tile: the next prompt's rows (or nothing) were loaded there,
 //                   and an infinity or a NaN must not meet a zero probability.  (Its keys are masked like those of later tokens.)
 // TMEM columns: S [0,128)  P_A [128,192)  P_B [192,256)  O_A [256,384)  O_B [384,512).
-// Bound: the key loop, tensor and exponential pipes in turns (one prompt of 16384 tokens: 80 % of a library product's rate).
+// Bound: the key loop, tensor and exponential pipes 63 % busy each, taken in turns (one prompt of 16384 tokens, 32 / 8 heads, d = 128
+// 1620 us: 1360 TFLOP/s, a library product's burst rate 1688, under the power cap 1389); short prompts: the chain of a unit.
 // grid min(148, units), block 384, dynamic smem 6 * (D/64) * 16 KB + 33 KB.
 struct SmemPrompt {
   uint64_t q_full, q_empty, kv_full[4], kv_empty[4], s_full[2], s_free, p_half[2][2], pv_done[2], v_tail, mma_done[2];
@@ -59,12 +63,12 @@ __global__ void __launch_bounds__(kAttnThreads, 1) prompt_kernel(const __grid_co
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
   volatile int* abort_flag = sh.wait_ctl;
 
-  // the k-th unit of this CTA (-1: none), its piece, its key tiles
-  auto unit_of = [&](int k) {
-    const int u = k * gridDim.x + (k & 1 ? gridDim.x - 1 - blockIdx.x : blockIdx.x);
-    return u < p.n_units ? u : -1;
+  // The k-th unit of this CTA; the kv-head is inverted in the last one.  All CTAs' first ones stand in front, then each CTA's others
+  // side by side, then where those begin (so there is something to read, and not to use, behind the last).  Its key tiles.
+  auto unit_at = [&](int k) {
+    const int4* units = reinterpret_cast<const int4*>(p.items);
+    return units[k == 0 ? blockIdx.x : reinterpret_cast<const int*>(units + p.n_units)[blockIdx.x] + k - 1];
   };
-  auto piece_of = [&](int u) { return u < 0 ? make_int4(0, 0, 0, 0) : *reinterpret_cast<const int4*>(p.items + u / p.Hkv); };
   auto tiles_of = [&](const int4& it) { return (min((it.z + 2) * TOK, it.y) + 127) / 128; };
 
   if (threadIdx.x == 0) {
@@ -123,12 +127,11 @@ __global__ void __launch_bounds__(kAttnThreads, 1) prompt_kernel(const __grid_co
           }
         };
         int n = 0, v_tok = 0, v_g = 0;                         // key tiles so far; where the V tile that is still to come stands
-        int u = unit_of(0);
-        int4 it = piece_of(u);
-        for (int k = 0; u >= 0 && ok; ++k) {
-          const int u_next = unit_of(k + 1);
-          const int4 next = piece_of(u_next);
-          const int g = u % p.Hkv, T = tiles_of(it);
+        int4 it = unit_at(0);
+        for (int k = 0; ok; ++k) {
+          const bool more = it.w >= 0;
+          const int4 next = unit_at(k + 1);
+          const int g = more ? it.w : ~it.w, T = tiles_of(it);
           if (k == 0) load_q(0, it, g);
           for (int j = 0; j < T && ok; ++j, ++n) {
             load_tile(n, 0, it.x + j * 128, g);
@@ -136,7 +139,7 @@ __global__ void __launch_bounds__(kAttnThreads, 1) prompt_kernel(const __grid_co
             if (j == 0 && k > 0) load_q(k, it, g);             // (behind the last V of the unit before: that is wanted first)
             v_tok = it.x + j * 128; v_g = g;
           }
-          u = u_next;
+          if (!more) break;
           it = next;
         }
         if (n > 0 && ok) load_tile(n - 1, 1, v_tok, v_g);
@@ -154,11 +157,10 @@ __global__ void __launch_bounds__(kAttnThreads, 1) prompt_kernel(const __grid_co
         const uint32_t q_lo0 = smem_desc_lo(smem_u32(sQ), 16), k_lo0 = smem_desc_lo(smem_u32(ring), 16);   // K-major operands
         bool ok = true;
         int n = 0, s = 0;                                      // key tiles and S so far
-        int u = unit_of(0);
-        int4 it = piece_of(u);
-        for (int k = 0; u >= 0 && ok; ++k) {
-          const int u_next = unit_of(k + 1);
-          const int4 next = piece_of(u_next);
+        int4 it = unit_at(0);
+        for (int k = 0; ok; ++k) {
+          const bool more = it.w >= 0;
+          const int4 next = unit_at(k + 1);
           const int T = tiles_of(it);
           ok = mbar_wait(&sh.q_full, k & 1, abort_flag);
           for (int i = 0; i < 2 * T && ok; ++i, ++s) {
@@ -178,7 +180,7 @@ __global__ void __launch_bounds__(kAttnThreads, 1) prompt_kernel(const __grid_co
             if (t == 1) { mma_commit(&sh.kv_empty[slot]); ++n; }
           }
           if (ok) mma_commit(&sh.q_empty);
-          u = u_next;
+          if (!more) break;
           it = next;
         }
       }
@@ -190,11 +192,10 @@ __global__ void __launch_bounds__(kAttnThreads, 1) prompt_kernel(const __grid_co
         const uint32_t v_lo0 = smem_desc_lo(smem_u32(ring) + kSlots * TILE_BYTES, kSubTileBytes);   // MN-major operand
         bool ok = true;
         int n = 0, s = 0;                                      // key tiles and S so far (of the units before: s)
-        int u = unit_of(0);
-        int4 it = piece_of(u);
-        for (int k = 0; u >= 0 && ok; ++k) {
-          const int u_next = unit_of(k + 1);
-          const int4 next = piece_of(u_next);
+        int4 it = unit_at(0);
+        for (int k = 0; ok; ++k) {
+          const bool more = it.w >= 0;
+          const int4 next = unit_at(k + 1);
           const int T = tiles_of(it);
           const bool tail = T * 128 > it.y;
           for (int i = 0; i < 2 * T && ok; ++i) {
@@ -223,7 +224,7 @@ __global__ void __launch_bounds__(kAttnThreads, 1) prompt_kernel(const __grid_co
             if (t == 1) { mma_commit(&sh.kv_empty[kSlots + slot]); ++n; }
           }
           s += 2 * T;
-          u = u_next;
+          if (!more) break;
           it = next;
         }
       }
@@ -231,11 +232,10 @@ __global__ void __launch_bounds__(kAttnThreads, 1) prompt_kernel(const __grid_co
       // ---------------------------------------------------------------- values behind a prompt's end
       int n = 0;                                               // key tiles so far
       bool ok = true;
-      int u = unit_of(0);
-      int4 it = piece_of(u);
-      for (int k = 0; u >= 0 && ok; ++k) {
-        const int u_next = unit_of(k + 1);
-        const int4 next = piece_of(u_next);
+      int4 it = unit_at(0);
+      for (int k = 0; ok; ++k) {
+        const bool more = it.w >= 0;
+        const int4 next = unit_at(k + 1);
         const int T = tiles_of(it);
         n += T;
         if (T * 128 > it.y) {
@@ -251,7 +251,7 @@ __global__ void __launch_bounds__(kAttnThreads, 1) prompt_kernel(const __grid_co
             if (lane == 0) mbar_arrive(&sh.v_tail);
           }
         }
-        u = u_next;
+        if (!more) break;
         it = next;
       }
     }
@@ -282,9 +282,9 @@ __global__ void __launch_bounds__(kAttnThreads, 1) prompt_kernel(const __grid_co
     const uint32_t tmem_S = tmem + lane_addr, tmem_P = tmem + 128 + t * 64 + lane_addr, tmem_O = tmem + 256 + t * 128 + lane_addr;
     bool ok = true;
     int n = 0;                                                 // key tiles so far
-    int u = unit_of(0);
-    int4 it = piece_of(u);
-    for (int k = 0; u >= 0; ++k) {
+    int4 it = unit_at(0);
+    for (int k = 0;; ++k) {
+      const bool more = it.w >= 0;
       const int T = tiles_of(it);
       const int tok0 = (it.z + t) * TOK, tok = tok0 + r_tok;
       float m_ref = -INFINITY, l = 0.f;                        // reference maximum (log2 units) and row sum
@@ -293,7 +293,7 @@ __global__ void __launch_bounds__(kAttnThreads, 1) prompt_kernel(const __grid_co
         // Waits that gave up only skip the arithmetic: the turn barrier is passed on every path, once per key tile and warp.
         if (ok) ok = __all_sync(0xffffffffu, mbar_wait(&sh.s_full[t], n & 1, abort_flag));
         bool took_turn = false, told = false;
-        const bool hand_over = t == 0 || j + 1 < T || unit_of(k + 1) >= 0;   // the other group has a key tile left, here or in the next unit
+        const bool hand_over = t == 0 || j + 1 < T || more;   // the other group has a key tile left, here or in the next unit
         if (ok) do {
           tc_fence_after_sync();
           uint32_t sr[128];
@@ -384,14 +384,13 @@ __global__ void __launch_bounds__(kAttnThreads, 1) prompt_kernel(const __grid_co
         if (!told && hand_over) named_barrier_arrive(3 - t, 256);
       }
       // ---- the unit's rows
-      const int u_next = unit_of(k + 1);
-      const int4 next = piece_of(u_next);
+      const int4 next = unit_at(k + 1);
       ok = ok && mbar_wait(&sh.pv_done[t], (n - 1) & 1, abort_flag);
       ok = __all_sync(0xffffffffu, ok);                        // the TMEM accesses below are warp-wide
       if (ok) {
         tc_fence_after_sync();
         // (fewer than 2^31 rows; -1: the row is none of the prompt's)
-        const int row = r < rows && tok < it.y ? (it.x + tok) * p.Hq + u % p.Hkv * p.G + hh : -1;
+        const int row = r < rows && tok < it.y ? (it.x + tok) * p.Hq + (more ? it.w : ~it.w) * p.G + hh : -1;
         const float inv = 1.f / l;
         uint8_t* mine = stage + warp * 4096;
 #pragma unroll
@@ -421,7 +420,7 @@ __global__ void __launch_bounds__(kAttnThreads, 1) prompt_kernel(const __grid_co
         if (row >= 0 && p.lse) p.lse[row] = (m_ref + log2f(l)) * 0.6931471805599453f;
       }
       tc_fence_before_sync();                                  // O is read: the next unit's P, behind which its first P V comes
-      u = u_next;
+      if (!more) break;
       it = next;
     }
     tc_fence_before_sync();

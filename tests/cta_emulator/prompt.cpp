@@ -31,15 +31,19 @@ int main(int argc, char** argv) {
   int tokens = 0;
   for (std::string item; std::getline(ss, item, ',');) {
     const int n = atoi(item.c_str()), tiles = (n + TOK - 1) / TOK;
-    for (int t = 0; t < tiles; t += 2) items.push_back({tokens, n, t, std::min(2, tiles - t)});
+    for (int t = 0; t < tiles; t += 2)
+      for (int h = 0; h < Hkv; ++h) items.push_back({tokens, n, t, h});
     tokens += n;
   }
+  const int units = (int)items.size();
+  items.back().head = ~items.back().head;
+  items.push_back({1, 0, 0, 0});                           // where the units behind the first stand
   std::vector<int4> held(items.size());                    // (aligned as the kernel reads them)
   memcpy(held.data(), items.data(), items.size() * sizeof(int4));
   std::vector<char> ws(256);
   std::vector<__nv_bfloat16> out((size_t)tokens * G * Hkv * 64 + 16);
   std::vector<float> lse((size_t)tokens * G * Hkv, -1.f);   // (its rows tell which were written)
-  kvc::PromptGeom g{G, G * Hkv, Hkv, (int)items.size() * Hkv, 1.f, num("limit_ms", 20) * 1000000 / 1024, reinterpret_cast<kvc::PromptItem*>(held.data()), lse.data()};
+  kvc::PromptGeom g{G, G * Hkv, Hkv, units, 1.f, num("limit_ms", 20) * 1000000 / 1024, reinterpret_cast<kvc::PromptItem*>(held.data()), lse.data()};
   CUtensorMap tm;
   memset(&tm, 0, sizeof(tm));
   const int rc = emu::run(kvc::kAttnThreads, [&] { kvc::prompt_kernel<64>(tm, tm, tm, out.data(), ws.data(), g); });

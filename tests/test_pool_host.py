@@ -88,7 +88,10 @@ def test_a_plan_covers_every_row_once_longest_first(dtype, hq, hkv, lens):
     plan = KvcPromptPlan()
     arr = (ctypes.c_int * len(lens))(*lens)
     assert lib.kvc_pool_plan(h, arr, len(lens), ctypes.byref(plan), None) == KVC_OK
-    assert (plan.n_seqs, plan.n_tokens, plan.item_bytes) == (len(lens), sum(lens), 16 * plan.n_items)
+    units = plan.n_items * (1 if dtype == KVC_F32 else hkv)
+    ctas = min(units, 148)
+    held = 16 * units + (0 if dtype == KVC_F32 else -(-ctas // 4) * 16)
+    assert (plan.n_seqs, plan.n_tokens, plan.item_bytes) == (len(lens), sum(lens), held)
     buf = ctypes.create_string_buffer(plan.item_bytes + 16)
     assert lib.kvc_pool_plan(h, arr, len(lens), ctypes.byref(plan), buf) == KVC_OK
     assert buf.raw[plan.item_bytes:] == bytes(16)
@@ -98,17 +101,30 @@ def test_a_plan_covers_every_row_once_longest_first(dtype, hq, hkv, lens):
         if n:
             starts[first] = n
         first += n
-    seen, work = set(), []
-    for first, n, tile, tiles in struct.iter_unpack("4i", buf.raw[:plan.item_bytes]):
-        assert starts[first] == n and tiles in ((1,) if dtype == KVC_F32 else range(1, plan.row_tiles + 1))
-        per = plan.row_tiles / G if dtype == KVC_F32 else 128 // G
-        for t in range(tile, tile + tiles):
-            assert t * per < n and (first, t) not in seen
-            seen.add((first, t))
-        work.append(-(-min(n, (tile + tiles) * per) // 128) * (1 if dtype == KVC_F32 else 1 + tiles))
-    rows = plan.row_tiles if dtype == KVC_F32 else (128 // G) * G
-    assert len(seen) == sum(-(-n * G // rows) for n in lens)
-    assert work == sorted(work, reverse=True)
+    entries = list(struct.iter_unpack("4i", buf.raw[:16 * units]))
+    per, step = (plan.row_tiles / G, 1) if dtype == KVC_F32 else (128 // G, 2)
+    tiles_of = {a: -(-n * G // plan.row_tiles) if dtype == KVC_F32 else -(-n // per) for a, n in starts.items()}
+    keys = lambda e: min(e[1], (e[2] + step) * per)  # noqa: E731
+    if dtype == KVC_F32:                                     # pieces for all kv-heads, those with the most keys first
+        want = {(a, t) for a in starts for t in range(tiles_of[a])}
+        work = [-(-min(e[1], -(-(e[2] + 1) * plan.row_tiles // G)) // 128) for e in entries]
+        assert work == sorted(work, reverse=True)
+        lists = [[(e[0], e[1], e[2])] for e in entries]
+    else:                                                    # a list per CTA, its first units in front, its last unit marked
+        others = list(struct.unpack(f"{ctas}i", buf.raw[16 * units:16 * units + 4 * ctas]))
+        assert others == sorted(others) and all(ctas <= x <= units for x in others)
+        want = {(a, t, g) for a in starts for t in range(0, tiles_of[a], step) for g in range(hkv)}
+        lists = [[entries[i]] + entries[others[i]:(others + [units])[i + 1]] for i in range(ctas)]
+        for x in lists:
+            assert [e[3] < 0 for e in x] == [False] * (len(x) - 1) + [True]
+        lists = [[(e[0], e[1], e[2], e[3] if e[3] >= 0 else ~e[3]) for e in x] for x in lists]
+        load = [sum(-(-keys(e) // 128) + 1 for e in x) for x in lists]
+        if load:                                             # nobody has more than one unit above the least
+            assert max(load) - min(load) <= max(-(-keys(e) // 128) + 1 for e in entries)
+    flat = [e for x in lists for e in x]
+    assert all(starts[e[0]] == e[1] for e in flat) and all(0 <= e[2] * per < e[1] for e in flat)
+    seen = [(e[0], e[2], *e[3:]) for e in flat]
+    assert len(seen) == len(set(seen)) and set(seen) == want
     assert lib.kvc_pool_destroy(h) == KVC_OK
 
 
