@@ -25,7 +25,7 @@ struct PromptGeom {
 // units sorted by length, without lists: 8 prompts of 383 - 4096, 32 / 8 heads, d = 128 256 us instead of 250, 300 + 2000 + 40 + 900,
 // 28 / 4 heads 44 - 49 instead of 39 - 41.)  While the softmax warps write a unit's rows, the next unit's Q, keys and values are already
 // there and its first S is computed.  With a CTA per unit (set-up, TMEM, first loads and the last stores in nobody's shadow) a unit of
-// one key tile cost 9 us, in a list it costs 3.5: 470 cycles to its S, 1170 for its maximum, 1800 for its weights, 700 for P V, 2500 for
+// one key tile cost 10 us (64 prompts of 128 tokens 69 us), in a list it costs 3.5: 470 cycles to its S, 1170 for its maximum, 1800 for its weights, 700 for P V, 2500 for
 // its rows.
 //   warps 0-3, 4-7  softmax of row tile A, B (216 registers); a warp's rows leave through a stage of its own, 64 columns at a time, as
 //                   whole lines (Q's shared memory is the next unit's by then; 32 bytes of 32 rows per store, straight from
@@ -97,7 +97,6 @@ __global__ void __launch_bounds__(kAttnThreads, 1) prompt_kernel(const __grid_co
   tc_fence_after_sync();
   const uint32_t tmem = sh.tmem_base;
   pdl_wait();
-  pdl_launch_dependents();
 
   if (warp >= 8) {
     reg_dec<56>();
