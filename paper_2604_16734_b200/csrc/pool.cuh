@@ -4,7 +4,7 @@
 // All of them, and those of packed prompts, are launched with programmatic stream serialization: they are brought up while the kernel
 // before them ends, wait for its end before they touch memory, and then let the next one be brought up (the bf16 prompts, which hold all
 // of an SM's shared and tensor memory, only by ending: 24 short prompts 13.2 us back to back, 13.6 with the others' call; one after another, against plain launches: 192 tokens
-// written 4.1 -> 2.8 us, one short sequence decoded 8.2 -> 6.3, 1225 + 24 tokens 10.8 -> 9.5, 64 sequences of 845 in 8 bits
+// written 4.1 -> 2.8 us, one short sequence decoded 8.2 -> 6.3, eight of up to 251, 32 / 32 heads 10.8 -> 9.5, 192 of up to 4500 in 8 bits
 // 101.6 -> 100.7).  What a kernel reads is no `const __restrict__`: such loads may be moved in front of the wait.
 #pragma once
 #include "geom.cuh"
@@ -118,7 +118,7 @@ __device__ __forceinline__ void put_row(char* codes, float* scales, long long ds
 // ------------------------------------------------------------------------------------------------
 // Rows -> pages and back.  A row is held by `kLanes` lanes, two 16-byte pieces each, kLanes apart; a block takes tokens of one
 // kv-head, so that its side of the pages is contiguous, and the kv-heads of the same tokens follow one another, so that the other
-// side is too.  Bound: HBM, at 5.6 - 5.7 TB/s of 6.45 for a copy (54000 tokens, 8 kv-heads, d = 128: bf16 into 8 bits 42 us with
+// side is too.  Bound: HBM, at 5.6 - 5.7 TB/s of 6.45 for a copy (38000 tokens, 8 kv-heads, d = 128: bf16 into 8 bits 42 us with
 // two rows in flight per thread, 45 with one, 52 with four; back 41 with one, 43 with two, 52 with four).
 static constexpr int kPoolThreads = 256, kWriteRows = 2, kReadRows = 1;
 template <typename T, int D> struct RowShape {
@@ -296,6 +296,10 @@ __global__ void __launch_bounds__(kPoolThreads) pool_read_kernel(const char* blo
 // Probabilities are rounded to the type of the values' product: bf16 as in the attention of a block (2^-9 each, of the
 // size of the output's own rounding), fp16 2^-12, and fp32 in two parts.
 // fp32 pages: three products of TF32 parts (x = hi + lo: hi hi + hi lo + lo hi, 2^-21 and below), sums in fp32.
+//
+// Measured: one sequence of 131k, 32 / 8 heads, d = 128, bf16 88.9 us, 6.04 TB/s (a copy: 6.45); 64 sequences to 4600
+// 100.3 us, 5.8 TB/s; 192 sequences to 4500, 28 / 4 heads, in 8 bits 98 - 101.6 us, 5.0 TB/s, where half of the issue slots are taken
+// too; one sequence of 128, fp32, 4 / 1 heads 6.3 us: lengths, table, rows, products and join, a chain of trips to L2.
 
 static constexpr int kDecodeMaxSeqs = 1024;                 // the sequences' tile counts are kept in shared memory
 static constexpr int kDecodeSmem = 232448 - 512 - (kDecodeMaxSeqs + 1) * 4 - kDecodeMaxSeqs;   // for the warps' rings and pieces
@@ -318,6 +322,8 @@ struct DecodeShape {
   template <int N> static __host__ __device__ constexpr int keys() { return N == 2 || (F32 && D == 128) ? 16 : 32; }
   template <int N> static __host__ __device__ constexpr int stage() { return keys<N>() * (2 * ROWB + (I8 ? 8 : 0)); }   // K, V, scales of both
   template <int N> static __host__ __device__ constexpr int piece() { return 8 * N * (D + 8) * 4; }
+  // Warps: what registers (65536) and rings leave room for.  8 bits, d = 128, tiles of 32: 8 warps 98 - 104 us for 192 sequences, 12 with
+  // tiles of 16 107, of 32 111; 10 warps would get 168 registers and spill (110).
   template <int N> static __host__ __device__ constexpr int warps() {
     return F32 && D == 128 ? 5 : N == 2 ? 8 : I8 ? 8 : D == 128 ? 6 : F32 ? 6 : 8;
   }

@@ -36,7 +36,7 @@ struct PromptGeom {
 //                   and an infinity or a NaN must not meet a zero probability.  (Its keys are masked like those of later tokens.)
 // TMEM columns: S [0,128)  P_A [128,192)  P_B [192,256)  O_A [256,384)  O_B [384,512).
 // Bound: the key loop, tensor and exponential pipes 63 % busy each, taken in turns (one prompt of 16384 tokens, 32 / 8 heads, d = 128
-// 1620 us: 1360 TFLOP/s, a library product's burst rate 1688, under the power cap 1389); short prompts: the chain of a unit.
+// 1620 us: 1360 TFLOP/s, a library product's burst rate 1645, under the power cap 1389); short prompts: the chain of a unit.
 // grid min(148, units), block 384, dynamic smem 6 * (D/64) * 16 KB + 33 KB.
 struct SmemPrompt {
   uint64_t q_full, q_empty, kv_full[4], kv_empty[4], s_full[2], s_free, p_half[2][2], pv_done[2], v_tail, mma_done[2];
