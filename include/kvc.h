@@ -374,6 +374,7 @@ typedef struct {
   long long n_tokens;  /* rows of q, k, v and out             */
   int n_items;         /* pieces of work                       */
   int row_tiles;       /* row tiles per piece (bf16), rows per piece (fp32)  */
+  int n_q_heads, n_kv_heads; /* the pool's: a plan serves pools of these heads and of its dtype */
   size_t item_bytes;   /* bytes of the items                   */
 } kvc_prompt_plan;
 int kvc_pool_plan(kvc_pool* pool, const int* lens, int n_seqs, kvc_prompt_plan* plan, void* items);

@@ -55,7 +55,7 @@ class KvcPoolConfig(ctypes.Structure):
 
 class KvcPromptPlan(ctypes.Structure):
     _fields_ = [("n_seqs", ctypes.c_int), ("n_tokens", ctypes.c_longlong), ("n_items", ctypes.c_int),
-                ("row_tiles", ctypes.c_int), ("item_bytes", ctypes.c_size_t)]
+                ("row_tiles", ctypes.c_int), ("n_q_heads", ctypes.c_int), ("n_kv_heads", ctypes.c_int), ("item_bytes", ctypes.c_size_t)]
 
 
 def lib_path() -> str:

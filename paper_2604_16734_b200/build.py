@@ -69,7 +69,7 @@ def build_calls(force: bool = False) -> str:
     cmd = [gxx, "-O2", "-std=c++17", "-shared", "-fPIC", "-fvisibility=hidden", "-w", f"-D_GLIBCXX_USE_CXX11_ABI={int(torch.compiled_with_cxx11_abi())}"]
     cmd += [f"-I{p}" for p in include_paths() + [os.path.join(cuda, "include"), sysconfig.get_paths()["include"]]]
     cmd += [os.path.join(CSRC, "pool_calls.cpp"), "-o", tmp] + [f"-L{p}" for p in library_paths()]
-    cmd += ["-ltorch_python", "-ltorch_cpu", "-lc10_cuda", "-lc10"]
+    cmd += ["-ltorch_python", "-ltorch_cpu", "-ltorch_cuda", "-lc10_cuda", "-lc10"]
     r = subprocess.run(cmd, capture_output=True, text=True)
     if r.returncode != 0:
         sys.stderr.write(r.stdout + r.stderr)

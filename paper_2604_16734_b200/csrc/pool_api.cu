@@ -340,6 +340,8 @@ extern "C" int kvc_pool_plan(kvc_pool* c, const int* lens, int n_seqs, kvc_promp
   plan->n_tokens = tokens;
   plan->n_items = (int)n_items;
   plan->row_tiles = R;
+  plan->n_q_heads = c->cfg.n_q_heads;
+  plan->n_kv_heads = c->cfg.n_kv_heads;
   plan->item_bytes = (size_t)plan_bytes(c, n_items);
   if (!items || n_items == 0) return KVC_OK;
   PromptItem* it = f32 ? (PromptItem*)items : new (std::nothrow) PromptItem[n_items];
@@ -406,7 +408,7 @@ extern "C" int kvc_pool_prompt(kvc_pool* c, const void* q, long long q_stride, c
   const kvc_pool_config& cf = c->cfg;
   if (!plan || !workspace) return fail(c, KVC_EINVAL, "null pointer argument");
   const bool f32 = cf.dtype == KVC_F32;
-  if (plan->n_tokens < 0 || plan->n_items < 0 || (long long)plan->n_items * cf.n_kv_heads > 0x7fffffffll || plan->n_tokens * cf.n_q_heads > 0x7fffffffll || plan->item_bytes != (size_t)plan_bytes(c, plan->n_items) ||
+  if (plan->n_q_heads != cf.n_q_heads || plan->n_kv_heads != cf.n_kv_heads || plan->n_tokens < 0 || plan->n_items < 0 || (long long)plan->n_items * cf.n_kv_heads > 0x7fffffffll || plan->n_tokens * cf.n_q_heads > 0x7fffffffll || plan->item_bytes != (size_t)plan_bytes(c, plan->n_items) ||
       (f32 ? plan->row_tiles != 64 && plan->row_tiles != 32 : plan->row_tiles != 2))
     return fail(c, KVC_EINVAL, "the plan is not one of this pool's");
   if (plan->n_tokens > 0 && (!q || !k || !v || !items || !out)) return fail(c, KVC_EINVAL, "null pointer argument");

@@ -71,7 +71,8 @@ def test_refusals_before_a_device_is_touched():
                 dict(qs=1016), dict(qs=1025), dict(ks=255)):
         a = {**pro, **bad}
         assert lib.kvc_pool_prompt(h, a["q"], a["qs"], a["k"], a["v"], a["ks"], ctypes.byref(plan), a["items"], a["ws"], a["out"], a["lse"], None) == KVC_EINVAL, bad
-    for field, value in (("n_tokens", -1), ("n_items", -1), ("row_tiles", 3), ("item_bytes", 0), ("n_tokens", 2 ** 31)):
+    for field, value in (("n_tokens", -1), ("n_items", -1), ("row_tiles", 3), ("item_bytes", 0), ("n_tokens", 2 ** 31), ("n_q_heads", 4),
+                         ("n_kv_heads", 1)):
         other = KvcPromptPlan.from_buffer_copy(plan)
         setattr(other, field, value)
         assert lib.kvc_pool_prompt(h, P, 1024, P, P, 256, ctypes.byref(other), P, P, P, P, None) == KVC_EINVAL, field
