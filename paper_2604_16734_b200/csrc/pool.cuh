@@ -297,9 +297,9 @@ __global__ void __launch_bounds__(kPoolThreads) pool_read_kernel(const char* blo
 // size of the output's own rounding), fp16 2^-12, and fp32 in two parts.
 // fp32 pages: three products of TF32 parts (x = hi + lo: hi hi + hi lo + lo hi, 2^-21 and below), sums in fp32.
 //
-// Measured: one sequence of 131k, 32 / 8 heads, d = 128, bf16 88.9 us, 6.04 TB/s (a copy: 6.45); 64 sequences to 4600
-// 100.3 us, 5.8 TB/s; 192 sequences to 4500, 28 / 4 heads, in 8 bits 98 - 101.6 us, 5.0 TB/s, where half of the issue slots are taken
-// too; one sequence of 128, fp32, 4 / 1 heads 6.3 us: lengths, table, rows, products and join, a chain of trips to L2.
+// Measured: one sequence of 131k, 32 / 8 heads, d = 128, bf16 87.3 us, 6.15 TB/s (a copy: 6.45); 64 sequences to 4600
+// 97.8 us, 5.97 TB/s; 192 sequences to 4500, 28 / 4 heads, in 8 bits 97.7 us, 5.17 TB/s, where half of the issue slots are taken
+// too; one sequence of 128, fp32, 4 / 1 heads 5.6 us: lengths, table, rows, products and join, a chain of trips to L2.
 
 static constexpr int kDecodeMaxSeqs = 1024;                 // the sequences' tile counts are kept in shared memory
 static constexpr int kDecodeSmem = 232448 - 512 - (kDecodeMaxSeqs + 1) * 4 - kDecodeMaxSeqs;   // for the warps' rings and pieces
@@ -335,7 +335,7 @@ struct DecodeShape {
   template <int N> static __host__ __device__ constexpr int warp_bytes() { return (stages<N>() * stage<N>() + OWN + piece<N>() + 127) / 128 * 128; }
 };
 static constexpr int kDecodeMaxCtas = kNumSMs;
-// A head's row of a piece: O in D floats, then m, l, and for the join the piece's factor and the joined m and l.
+// A head's row of a piece: O in D floats, then m and l (and room, so that rows begin eight banks apart).
 __host__ __device__ constexpr int decode_row(int D) { return D + 8; }
 static constexpr int kDecodePieceFloats = 16 * (128 + 8);   // a piece in the workspace: up to 16 heads
 
@@ -792,29 +792,39 @@ __global__ void __launch_bounds__(DecodeShape<T, D, I8>::template warps<NT>() * 
 
   // ---- the line of work (the host has checked that it has fewer than 2^31 tiles)
   const int room = static_cast<int>((static_cast<long long>(table_stride) << p.ps_log2) - (k_new ? 1 : 0));
-  if (threadIdx.x < kDecodeWarps * 2) s_seg[threadIdx.x >> 1][threadIdx.x & 1] = -1;
+  if (lane < 2) s_seg[warp][lane] = -1;
   if (threadIdx.x == 0) pre[0] = 0;
   pdl_wait();
   pdl_launch_dependents();
-  int sum = 0;
-  for (int i0 = 0; i0 < n_seqs; i0 += kDecodeThreads) {
-    const int i = i0 + threadIdx.x;
-    int x = 0;
-    if (i < n_seqs) {
-      int len = lens[i];
-      if (len < 0 || len > room) { if (blockIdx.x == 0) pool_refuse(ws); len = len < 0 ? 0 : room; }
-      if (k_new) ++len;                                      // rows of the sequence, its new one included
-      x = (len + TK - 1) / TK;
-      last[i] = static_cast<uint8_t>((len - 1) & (TK - 1)) + 1;
-    }
+  auto tiles_of = [&](int i) {                               // tiles of sequence i, and the rows of its last one
+    int len = lens[i];
+    if (len < 0 || len > room) { if (blockIdx.x == 0) pool_refuse(ws); len = len < 0 ? 0 : room; }
+    if (k_new) ++len;                                        // rows of the sequence, its new one included
+    last[i] = static_cast<uint8_t>((len - 1) & (TK - 1)) + 1;
+    return (len + TK - 1) / TK;
+  };
+  auto scan = [&](int x) {
 #pragma unroll
     for (int o = 1; o < 32; o <<= 1) { const int y = __shfl_up_sync(0xffffffffu, x, o); if (lane >= o) x += y; }
-    if (lane == 31) s_scan[warp] = x;
-    __syncthreads();
-    int before = sum;
-    for (int w = 0; w < kDecodeWarps; ++w) { if (w < warp) before += s_scan[w]; sum += s_scan[w]; }
-    if (i < n_seqs) pre[i + 1] = before + x;
-    __syncthreads();
+    return x;
+  };
+  int sum = 0;
+  if (n_seqs <= 32) {                                        // every warp for itself (all write the same): two barriers, 0.05 - 0.1 us, less
+    const int x = scan(lane < n_seqs ? tiles_of(lane) : 0);
+    sum = __shfl_sync(0xffffffffu, x, 31);
+    if (lane < n_seqs) pre[lane + 1] = x;
+    if (lane == 0) pre[0] = 0;
+    __syncwarp();
+  } else {
+    for (int i0 = 0; i0 < n_seqs; i0 += kDecodeThreads) {
+      const int i = i0 + threadIdx.x, x = scan(i < n_seqs ? tiles_of(i) : 0);
+      if (lane == 31) s_scan[warp] = x;
+      __syncthreads();
+      int before = sum;
+      for (int w = 0; w < kDecodeWarps; ++w) { if (w < warp) before += s_scan[w]; sum += s_scan[w]; }
+      if (i < n_seqs) pre[i + 1] = before + x;
+      __syncthreads();
+    }
   }
   const int total = sum * HH;
   const int per = max((total + static_cast<int>(gridDim.x) - 1) / static_cast<int>(gridDim.x), p.min_keys / TK);
@@ -855,7 +865,7 @@ __global__ void __launch_bounds__(DecodeShape<T, D, I8>::template warps<NT>() * 
     const int rel = x0 - pre[cur.seq] * HH;
     const int hh = rel / cur.tiles;
     cur.t = rel - hh * cur.tiles;
-    cur.g = hh / HG;
+    cur.g = HG == 1 ? hh : hh / HG;
     cur.hg = hh - cur.g * HG;
   }
   auto step = [&](Cursor& x) {                               // on to the next tile
@@ -914,19 +924,24 @@ __global__ void __launch_bounds__(DecodeShape<T, D, I8>::template warps<NT>() * 
         int own = TK;
         const char* k_own = nullptr;
         const char* v_own = nullptr;
+        uint4 kr, vr;
+        long long to = -1;
+        const int piece = lane % LANES;
+        float* sc = reinterpret_cast<float*>(own_codes + 2 * D);
         if (k_new && end && (rows > 16 ? ok2 : ok)) {        // (every head group writes the same bytes)
           own = rows - 1;
           const long long src = ld.seq * kv_stride + static_cast<long long>(ld.g) * D;
           k_own = reinterpret_cast<const char*>(k_new + src);
           v_own = reinterpret_cast<const char*>(v_new + src);
-          const int piece = lane % LANES;
-          const long long to = lane >= LANES ? -1ll : own < 16 ? static_cast<long long>(row) + own : static_cast<long long>(row2) + own - 16;
-          const uint4 kr = reinterpret_cast<const uint4*>(k_own)[piece], vr = reinterpret_cast<const uint4*>(v_own)[piece];
-          float* sc = reinterpret_cast<float*>(own_codes + 2 * D);
+          to = lane >= LANES ? -1ll : own < 16 ? static_cast<long long>(row) + own : static_cast<long long>(row2) + own - 16;
+          kr = reinterpret_cast<const uint4*>(k_own)[piece];
+          vr = reinterpret_cast<const uint4*>(v_own)[piece];
+        }
+        auto put = [&]() {
           put_row<T, D, I8>(blob, reinterpret_cast<float*>(blob + p.ks_off), to, piece, kr, own_codes, sc);
           put_row<T, D, I8>(blob + p.v_off, reinterpret_cast<float*>(blob + p.vs_off), to, piece, vr, own_codes + D, sc + 1);
-          __syncwarp();
-        }
+        };
+        if (I8 && own < TK) { put(); __syncwarp(); }         // (its codes are wanted now)
 #pragma unroll 1
         for (int h = 0; h < TK / 16; ++h) {
           const bool there = h ? ok2 : ok;
@@ -936,6 +951,7 @@ __global__ void __launch_bounds__(DecodeShape<T, D, I8>::template warps<NT>() * 
           Dec::template load<false>(stage, h, k_lane + at * S::ROWB, v_lane + at * S::ROWB, s_lane + at * 4, lim, mine, k_own, v_own, own_codes);
         }
         if (I8 && own < TK) __syncwarp();                    // (the next own row may be written over this one)
+        if (!I8 && own < TK) put();                          // (the tile's loads do not wait for this row's: 0.2 us of 6)
       }
       if (++ld_stage == NS) ld_stage = 0;
       step(ld);
@@ -1022,29 +1038,12 @@ __global__ void __launch_bounds__(DecodeShape<T, D, I8>::template warps<NT>() * 
     store4<T>(out + to * D + d4 * 4, make_float4(o.x * inv, o.y * inv, o.z * inv, o.w * inv));
     if (lse && d4 == 0) lse[to] = l != 0.f ? (m + log2f(l)) * 0.6931471805599453f : -INFINITY;
   };
-  // Every warp sees the pieces' segments; pieces of one segment are a group.
+  // Every warp sees the pieces' segments; pieces of one segment are a group.  A thread takes four channels of a head and works out the
+  // pieces' factors itself (by a thread per piece and head first, and a barrier: 0.3 us more of 6 - 13).
   constexpr int P = 2 * kDecodeWarps;
   static_assert(P <= 32);
   const int seg_l = lane < P ? (&s_seg[0][0])[lane] : -1;
   const uint32_t group_l = __match_any_sync(0xffffffffu, seg_l);
-  // factors: a thread per (piece, head)
-  for (int y = threadIdx.x; y < (P * H + 31) / 32 * 32; y += kDecodeThreads) {      // (whole warps, for the shuffles)
-    const int k = min(y / H, P - 1), h = y % H;
-    const uint32_t group = __shfl_sync(0xffffffffu, group_l, k);
-    if (__shfl_sync(0xffffffffu, seg_l, k) < 0 || y >= P * H) continue;
-    float mk[P], m = -INFINITY, l = 0.f;
-#pragma unroll
-    for (int i = 0; i < P; ++i) { mk[i] = group >> i & 1u ? piece_at(i)[h * RS + D] : -INFINITY; m = fmaxf(m, mk[i]); }
-#pragma unroll
-    for (int i = 0; i < P; ++i)
-      if (group >> i & 1u) l = fmaf(mk[i] == -INFINITY ? 0.f : fast_exp2(mk[i] - m), piece_at(i)[h * RS + D + 1], l);
-    float* row = piece_at(k) + h * RS;
-    const float own = row[D];
-    row[D + 2] = own == -INFINITY ? 0.f : fast_exp2(own - m);
-    row[D + 3] = m;
-    row[D + 4] = l;
-  }
-  __syncthreads();
   int open_seg[2] = {-1, -1}, open_c0[2] = {0, 0}, open_n[2] = {0, 0};     // segments of several CTAs: the one that ends here, the one that begins here
   for (uint32_t left = __ballot_sync(0xffffffffu, seg_l >= 0); left;) {
     const int first = __ffs(left) - 1, seg = __shfl_sync(0xffffffffu, seg_l, first);
@@ -1057,16 +1056,19 @@ __global__ void __launch_bounds__(DecodeShape<T, D, I8>::template warps<NT>() * 
     float* joint = joints + (static_cast<long long>(blockIdx.x) * 2 + which) * kDecodePieceFloats;
     for (int y = threadIdx.x; y < heads * (D / 4); y += kDecodeThreads) {
       const int h = y / (D / 4), d4 = y % (D / 4);
+      float mk[P], m = -INFINITY, l = 0.f;
+#pragma unroll
+      for (int i = 0; i < P; ++i) { mk[i] = group >> i & 1u ? piece_at(i)[h * RS + D] : -INFINITY; m = fmaxf(m, mk[i]); }
       float4 o = make_float4(0.f, 0.f, 0.f, 0.f);
 #pragma unroll
       for (int i = 0; i < P; ++i)
         if (group >> i & 1u) {
           const float* src = piece_at(i) + h * RS;
           const float4 v = *reinterpret_cast<const float4*>(src + d4 * 4);
-          const float f = src[D + 2];
+          const float f = mk[i] == -INFINITY ? 0.f : fast_exp2(mk[i] - m);
+          l = fmaf(f, src[D + 1], l);
           o.x = fmaf(f, v.x, o.x); o.y = fmaf(f, v.y, o.y); o.z = fmaf(f, v.z, o.z); o.w = fmaf(f, v.w, o.w);
         }
-      const float m = piece_at(first)[h * RS + D + 3], l = piece_at(first)[h * RS + D + 4];
       if (complete) {
         give(sq, hh, h, d4, o, m, l);
       } else {
