@@ -775,7 +775,7 @@ __global__ void __launch_bounds__(DecodeShape<T, D, I8>::template warps<NT>() * 
   constexpr int H = 8 * NT, RS = decode_row(D), LANES = D / Piece<T>::N, NS = S::template stages<NT>(), STAGE = S::template stage<NT>(), TK = Dec::TK,
                 WB = S::template warp_bytes<NT>();
   constexpr int kDecodeWarps = S::template warps<NT>(), kDecodeThreads = kDecodeWarps * 32;
-  static_assert(kDecodeWarps * WB >= (kDecodeMaxCtas + 1) * H * 8 + kDecodeThreads * 16, "the last join");
+  static_assert(kDecodeWarps * WB >= kDecodeThreads * 24, "the last join");
   static_assert(NS >= 2 && NS * STAGE >= S::template piece<NT>(), "two tiles on their way; the last piece overlays the ring");
   extern __shared__ __align__(128) uint8_t smem_b[];          // per warp: ring, own row, first piece; then the line of work
   int* pre = reinterpret_cast<int*>(smem_b + kDecodeWarps * WB);           // [n_seqs + 1] tiles of one head before a sequence
@@ -1088,10 +1088,11 @@ __global__ void __launch_bounds__(DecodeShape<T, D, I8>::template warps<NT>() * 
     const int seg = threadIdx.x ? open_seg[1] : open_seg[0], n = threadIdx.x ? open_n[1] : open_n[0];
     int last_one = 0;
     if (seg >= 0) {
-      __threadfence();                                       // (what the block has written before the barrier goes first)
-      last_one = atomicAdd(counters + seg, 1) == n - 1;
+      // (releases what the block has written before the barrier, acquires what the others released: cheaper than two __threadfence)
+      int before;
+      asm volatile("atom.acq_rel.gpu.global.add.s32 %0, [%1], 1;" : "=r"(before) : "l"(counters + seg) : "memory");
+      last_one = before == n - 1;
       if (last_one) counters[seg] = 0;                       // as it was found
-      __threadfence();
     }
     s_last[threadIdx.x] = last_one;
   }
@@ -1101,60 +1102,64 @@ __global__ void __launch_bounds__(DecodeShape<T, D, I8>::template warps<NT>() * 
     if (!s_last[w]) continue;
     const int seg = w ? open_seg[1] : open_seg[0], c0 = w ? open_c0[1] : open_c0[0], n = w ? open_n[1] : open_n[0];
     const int sq = seg / HH, hh = seg - sq * HH, heads = min(H, p.G - hh % HG * H);
-    // (shared memory of the rings, which nobody uses any more: factors [n][heads], joined (m, l) [heads], sums of parts)
-    float2* ml = reinterpret_cast<float2*>(smem_b);
-    float2* all = ml + kDecodeMaxCtas * H;
-    float4* sums = reinterpret_cast<float4*>(all + H);
+    // (shared memory of the rings, which nobody uses any more: sums of parts, and their m and l)
+    float4* sums = reinterpret_cast<float4*>(smem_b);
+    float2* sums_ml = reinterpret_cast<float2*>(sums + kDecodeThreads);
     auto piece = [&](int k) { return joints + (static_cast<long long>(c0 + k) * 2 + (k == 0)) * kDecodePieceFloats; };
     const int rows = heads * (D / 4), parts = max(1, min(kDecodeThreads / rows, n));
-    const int part = parts > 1 ? threadIdx.x / rows : 0;
+    const int part = parts > 1 ? threadIdx.x / rows : 0, y_first = threadIdx.x - part * rows;
     constexpr int kBatch = 8;                                // loads of a thread on their way: a trip to L2 takes 900 cycles
-    float4 v[kBatch];
-    auto fetch = [&](int y, int k0) {
-#pragma unroll
-      for (int i = 0; i < kBatch; ++i) {
-        const int k = k0 + i * parts;
-        v[i] = y < rows && k < n ? __ldcg(reinterpret_cast<const float4*>(piece(k) + y / (D / 4) * RS + y % (D / 4) * 4)) : make_float4(0.f, 0.f, 0.f, 0.f);
-      }
-    };
-    const int y_first = parts > 1 ? (part < parts ? static_cast<int>(threadIdx.x) - part * rows : rows) : threadIdx.x;
-    fetch(y_first, part);                                    // (before the factors are known)
-    for (int y = threadIdx.x; y < n * heads; y += kDecodeThreads) ml[y] = __ldcg(reinterpret_cast<const float2*>(piece(y / heads) + y % heads * RS + D));
-    __syncthreads();
-    for (int h = warp; h < heads; h += kDecodeWarps) {
-      float m = -INFINITY, l = 0.f;
-      for (int k = lane; k < n; k += 32) m = fmaxf(m, ml[k * heads + h].x);
-#pragma unroll
-      for (int o = 16; o > 0; o >>= 1) m = fmaxf(m, __shfl_xor_sync(0xffffffffu, m, o));
-      for (int k = lane; k < n; k += 32) {
-        const float2 x = ml[k * heads + h];
-        const float f = x.x == -INFINITY ? 0.f : fast_exp2(x.x - m);
-        l = fmaf(f, x.y, l);
-        ml[k * heads + h].x = f;
-      }
-#pragma unroll
-      for (int o = 16; o > 0; o >>= 1) l += __shfl_xor_sync(0xffffffffu, l, o);
-      if (lane == 0) all[h] = make_float2(m, l);
-    }
-    __syncthreads();
+#pragma unroll 1
     for (int y = y_first, round = 0; round * kDecodeThreads < rows; ++round, y += kDecodeThreads) {   // (one round, or one part)
+      const bool mine = y < rows && part < parts;
       const int h = min(y, rows - 1) / (D / 4), d4 = y % (D / 4);
       float4 o = make_float4(0.f, 0.f, 0.f, 0.f);
+      float m = -INFINITY, l = 0.f;
       for (int k0 = part; k0 < n; k0 += kBatch * parts) {
-        if (round > 0 || k0 > part) fetch(y, k0);
+        float4 v[kBatch];
+        float2 x[kBatch];
+        float top = m;
 #pragma unroll
         for (int i = 0; i < kBatch; ++i) {
-          const float f = ml[min(k0 + i * parts, n - 1) * heads + h].x;      // (times zero behind the last)
+          const int k = k0 + i * parts;
+          const bool there = mine && k < n;
+          const float* row = piece(there ? k : 0) + h * RS;
+          v[i] = there ? __ldcg(reinterpret_cast<const float4*>(row + d4 * 4)) : make_float4(0.f, 0.f, 0.f, 0.f);
+          x[i] = there ? __ldcg(reinterpret_cast<const float2*>(row + D)) : make_float2(-INFINITY, 0.f);
+        }
+#pragma unroll
+        for (int i = 0; i < kBatch; ++i) top = fmaxf(top, x[i].x);
+        const float f0 = m == -INFINITY ? 0.f : fast_exp2(m - top);
+        o.x *= f0; o.y *= f0; o.z *= f0; o.w *= f0;
+        l *= f0;
+        m = top;
+#pragma unroll
+        for (int i = 0; i < kBatch; ++i) {
+          const float f = x[i].x == -INFINITY ? 0.f : fast_exp2(x[i].x - m);
+          l = fmaf(f, x[i].y, l);
           o.x = fmaf(f, v[i].x, o.x); o.y = fmaf(f, v[i].y, o.y); o.z = fmaf(f, v[i].z, o.z); o.w = fmaf(f, v[i].w, o.w);
         }
       }
       if (parts > 1) {
-        if (y < rows && part > 0) sums[(part - 1) * rows + y] = o;
+        if (mine && part > 0) { sums[(part - 1) * rows + y] = o; sums_ml[(part - 1) * rows + y] = make_float2(m, l); }
         __syncthreads();
-        if (y < rows && part == 0)
-          for (int i = 0; i < parts - 1; ++i) { const float4 x = sums[i * rows + y]; o.x += x.x; o.y += x.y; o.z += x.z; o.w += x.w; }
+        if (mine && part == 0) {
+          float top = m;
+          for (int i = 0; i < parts - 1; ++i) top = fmaxf(top, sums_ml[i * rows + y].x);
+          const float f0 = m == -INFINITY ? 0.f : fast_exp2(m - top);
+          o.x *= f0; o.y *= f0; o.z *= f0; o.w *= f0;
+          l *= f0;
+          m = top;
+          for (int i = 0; i < parts - 1; ++i) {
+            const float4 v = sums[i * rows + y];
+            const float2 x = sums_ml[i * rows + y];
+            const float f = x.x == -INFINITY ? 0.f : fast_exp2(x.x - m);
+            l = fmaf(f, x.y, l);
+            o.x = fmaf(f, v.x, o.x); o.y = fmaf(f, v.y, o.y); o.z = fmaf(f, v.z, o.z); o.w = fmaf(f, v.w, o.w);
+          }
+        }
       }
-      if (y < rows && part == 0) give(sq, hh, h, d4, o, all[h].x, all[h].y);
+      if (mine && part == 0) give(sq, hh, h, d4, o, m, l);
     }
     __syncthreads();
   }
