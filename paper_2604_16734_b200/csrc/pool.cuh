@@ -19,7 +19,8 @@ struct PoolGeom {
   int ps_log2;                     // page size = 1 << ps_log2
   float scale_log2;                // softmax scale times log2(e)
   // Decode: fewest keys (of all segments) that a CTA gets, in whole tiles.  256, against 128 and 512: one sequence of 1000, 32 / 8
-  // heads, d = 128 10.2, 10.3, 11.4 us; sixteen of 100 - 700 12.0, 12.0, 14.6; four of 1500, 28 / 4 heads 13.2, 12.7, 14.3.
+  // heads, d = 128 10.2, 10.3, 11.4 us; sixteen of 100 - 700 12.0, 12.0, 14.6; four of 1500, 28 / 4 heads 13.2, 12.7, 14.3 (with an
+  // earlier join, a microsecond slower).
   int min_keys;
   long long v_off, ks_off, vs_off; // byte offsets inside a blob of V, K scales, V scales (K is at 0)
   long long joints_off;            // byte offset in the workspace of the pieces of segments that span CTAs
@@ -327,7 +328,7 @@ struct DecodeShape {
   template <int N> static __host__ __device__ constexpr int warps() {
     return F32 && D == 128 ? 5 : N == 2 ? 8 : I8 ? 8 : D == 128 ? 6 : F32 ? 6 : 8;
   }
-  template <int N> static __host__ __device__ constexpr int near() { return 98304 / stage<N>(); }   // (tiles; at its use)
+  template <int N> static __host__ __device__ constexpr int near() { return 65536 / stage<N>(); }   // (tiles; at its use)
   template <int N> static __host__ __device__ constexpr int stages() {
     const int n = (kDecodeSmem / warps<N>() / 128 * 128 - piece<N>() - OWN) / stage<N>();
     return n < 6 ? n : 6;
@@ -828,10 +829,10 @@ __global__ void __launch_bounds__(DecodeShape<T, D, I8>::template warps<NT>() * 
   }
   const int total = sum * HH;
   const int per = max((total + static_cast<int>(gridDim.x) - 1) / static_cast<int>(gridDim.x), p.min_keys / TK);
-  // Where the ranges are short, a boundary moves to an end of its segment that is near: joining pieces across CTAs costs about 3 us,
-  // as much as the loads of kNear tiles (96 KB).  Left out: one sequence of 2000, 28 / 4 heads, d = 128 13.0 -> 17.0 us, sixteen of
-  // 100 - 700, 32 / 8 heads in 8 bits 12.0 -> 17.0; twice as far 14.0, 12.0; half as far 11.7, 13.8, and one of 8000, 32 / 8 heads
-  // 13.6 -> 16.4.  (Where no boundary is near an end, the search costs 0.2 - 0.5 us.)
+  // Where the ranges are short, a boundary moves to an end of its segment that is near: joining pieces across CTAs costs about 2 us,
+  // as much as the loads of kNear tiles (64 KB).  Left out: one sequence of 2000, 28 / 4 heads, d = 128 10.0 -> 14.2 us, sixteen of
+  // 100 - 700, 32 / 8 heads in 8 bits 11.0 -> 14.7; with 48 KB four of 1500, 28 / 4 heads 10.3 -> 13.1, with 96 KB 11.1 (but one of
+  // 8000, 32 / 8 heads 14.0 -> 12.0).  (Where no boundary is near an end, the search costs up to 0.1 us.)
   constexpr int kNear = S::template near<NT>();
   const int near = per <= 4 * kNear ? kNear : 0;
   auto sequence_of = [&](int x) {                            // the sequence that holds tile x: the last whose tiles begin at or before it
